@@ -171,6 +171,47 @@ segattn_status segattn_layer_policy(int32_t n_kv_heads, const int32_t *long_head
 segattn_status seg_rope_apply(const segattn_config *cfg, void *q, void *k, int64_t rows,
                               const int64_t *pos0, void *stream);
 
+/* Rotary positions in the forms that models are trained with.  Pair i, i < rotary_dim / 2, of a head at
+ * position p is turned by the angle p * f_i and multiplied by `magnitude`:
+ *   (a, b) -> magnitude * (a cos - b sin, a sin + b cos).
+ * Without scaling f_i = theta^(-2i / rotary_dim).  For contexts longer than the trained ones the frequencies
+ * become f_i * (kept_i + (1 - kept_i) / factor) with
+ *   LINEAR        kept_i = 0 (all positions divided by factor);
+ *   BY_ROTATIONS  kept_i rises linearly from 0 to 1 while the rotations that pair i makes within trained_len
+ *                 positions, trained_len * f_i / (2 pi), rise from `low` to `high`;
+ *   BY_INDEX      kept_i falls linearly from 1 to 0 while the index i rises from that of the pair that makes
+ *                 `high` rotations (rounded down, not below 0) to that of the one that makes `low` (rounded
+ *                 up, not above rotary_dim - 1).
+ * Frequencies are formed and angles reduced in double precision. */
+enum { SEGATTN_ROPE_PLAIN = 0, SEGATTN_ROPE_LINEAR = 1, SEGATTN_ROPE_BY_ROTATIONS = 2, SEGATTN_ROPE_BY_INDEX = 3 };
+typedef struct {
+  double theta;          /* > 0 (BY_INDEX: not 1)                                                    */
+  int32_t rotary_dim;    /* channels of a head that are turned, from the first on: a multiple of 16
+                            up to D; 0 means D.  The others are passed on as they are                */
+  int32_t interleaved;   /* 0: pair i is channels i and i + rotary_dim / 2; 1: channels 2i and 2i + 1 */
+  int32_t scaling;       /* SEGATTN_ROPE_*                                                           */
+  double factor;         /* > 0; not used by PLAIN                                                   */
+  double trained_len;    /* > 0, low, high: BY_ROTATIONS and BY_INDEX only                           */
+  double low, high;      /* 0 < low < high                                                           */
+  double magnitude;      /* >= 0; 0 means 1                                                          */
+  const double *inv_freq;/* host, [rotary_dim / 2] or NULL: the f_i themselves, instead of theta and
+                            scaling (copied)                                                         */
+} segattn_rope;
+
+/* Turns q [B*rows,Hq,D] and k [B*rows,Hkv,D] into q_out and k_out (either pair may be NULL; in place where the
+ * pointers are the same).  Row t of sequence b is at position pos0[b] + t (device int64 [B]; NULL: all 0), or row
+ * j of all at pos[j] (device int64 [B*rows]: packed batches, caches that were evicted from; not both).  The
+ * strides are in elements between token rows, 0 for dense, so that q and k can be parts of one projection's
+ * output; heads are dense inside a row; rows and pointers on 16 bytes.  fp32 = 0: bf16, 1: float, in and out.
+ * Outputs must not overlap inputs otherwise.  inverse = 1 turns by the negative angles (and multiplies by the
+ * magnitude all the same): applied to the gradients of q_out and k_out it gives those of q and k, for bf16
+ * and fp32 results of seg_attn_bwd_* alike.  cfg's rope_theta is not used. */
+segattn_status seg_rope_rotate(const segattn_config *cfg, const segattn_rope *rope, const void *q,
+                               int64_t q_stride, const void *k, int64_t k_stride, int64_t rows,
+                               const int64_t *pos0, const int64_t *pos, int32_t inverse, int32_t fp32,
+                               void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride,
+                               void *stream);
+
 /* ---- backward (training) ---------------------------------------------------------------- */
 
 /* Gradients of seg_attn_fwd_seq for truncated backpropagation over segments (Sec. 3.2,
@@ -375,6 +416,88 @@ size_t segattn_resident_bytes(const segattn_ctx *ctx);
  * rule as seg_kv_commit).  ECAPACITY if a PAST pool would overflow. */
 segattn_status seg_attn_decode(segattn_ctx *ctx, const void *q, const void *k_new,
                                const void *v_new, void *out, float *lse, void *stream);
+
+/* ---- paged cache -------------------------------------------------------------------------
+ *
+ * Keys and values in pages of a pool that the caller owns, for programs that serve many sequences from one
+ * allocation.  No context: what a sequence holds is said by device arrays that the calls read and write in
+ * stream order, so a captured step can be replayed while the cache grows.
+ *   rows   int32 [B,Hkv]: rows that the (sequence, KV head) holds.  Row r of it is row r % page_rows of
+ *          the page that entry r / page_rows of its table names.
+ *   pages  page 0..n_pages-1 holds page_rows rows of every KV head, and table is int32 [B,max_pages]; or
+ *          (per_head) page_rows rows of one head, and table is int32 [B,Hkv,max_pages].  An entry outside
+ *          0..n_pages-1 names no page: rows there are not seen, not written and not moved.  A sequence's entries
+ *          behind its last row need not be set, nor those of a head without the PAST bit before its window.
+ * A head's policy keeps its meaning.  A head without the PAST bit sees the rows from max(0, s - T) on (TAIL)
+ * or from s on (SEG), where s is the start of the segment of the newest row, so its row numbers have to be the
+ * tokens' positions; a PAST head sees every row it holds (TAIL|PAST too), in any order.  The configuration's
+ * validation mode, retrieval mode, past_capacity and rope_theta do not apply here (the first two: EINVAL).
+ * Pages may be shared between sequences as long as nobody appends to, evicts from or accumulates weights of
+ * them: those calls change the page for everyone who names it, in no fixed order.
+ * The current device has to be the stream's and the pointers' (EINVAL for another device's stream). */
+enum { SEGATTN_PAGES_BF16 = 0, SEGATTN_PAGES_E4M3 = 1 };
+typedef struct {
+  void *k, *v;            /* device, 16-byte aligned: rows of D elements                             */
+  int32_t type;           /* bf16, or e4m3 (4 significant bits, largest 448, NaN, no infinity)       */
+  int32_t page_rows;      /* >= 1; multiples of 32 are fastest                                       */
+  int32_t n_pages;        /* in the pool                                                             */
+  int32_t max_pages;      /* entries of a table; max_pages * page_rows < 2^31 - 4096                 */
+  int32_t per_head;       /* 1: a page holds the rows of one KV head                                 */
+  int64_t page_stride;    /* of k and v, in elements, a multiple of 16 bytes: between pages,         */
+  int64_t head_stride;    /* between the heads of a page (not used with per_head)                    */
+  int64_t row_stride;     /* and between rows, >= D; all three 0: dense [n_pages][heads][page_rows][D] */
+  uint8_t *k_scale, *v_scale; /* e4m3: device [n_pages][heads][page_rows], heads = 1 with per_head:
+                             the row's elements times 2^(byte - 127), byte 1..254                     */
+  float *mass;            /* device, same layout, or NULL: attention weight a row has received        */
+  int32_t *pos;           /* device, same layout, or NULL: position of a row's token                  */
+  const int32_t *table;   /* device                                                                  */
+} segattn_pages;
+
+/* Appends the tokens k,v [total,Hkv,D] (dense bf16): sequence b's are rows cu_seqlens[b] .. cu_seqlens[b+1]-1
+ * (device int32 [B+1], ascending from 0; max_seqlen: the most of one sequence, total: all, host values), or NULL
+ * for one token per sequence (total = B, max_seqlen = 1).  They become rows rows[b,h] on of every KV head, and
+ * rows_out[b,h] = rows[b,h] + their number (rows_out may be rows).  Token i of a sequence is at position
+ * pos0[b] + i (device int64 [B]; NULL: all 0), which pos gets and, with a rope, the key is turned by; q
+ * [total,Hq,D] (NULL: none) is then turned into q_out (may be q).  Without a rope keys are taken as they are
+ * (and q is not needed).  mass, where there is one, starts at 0.  e4m3: a row is stored with the smallest
+ * power of two 2^e >= 2^-119 for which its largest finite magnitude is at most 448 * 2^e, every element rounded
+ * once to nearest even; what is not finite becomes NaN.  bf16: turned keys are rounded once.  A row that has
+ * no place (no page, or behind the table's last row) is dropped, and rows_out stops at the table's last row. */
+segattn_status seg_kv_paged_append(const segattn_config *cfg, const segattn_pages *pages,
+                                   const segattn_rope *rope, const void *q, const void *k, const void *v,
+                                   const int32_t *cu_seqlens, int64_t total, int64_t max_seqlen,
+                                   const int64_t *pos0, const int32_t *rows, void *q_out, int32_t *rows_out,
+                                   void *stream);
+
+/* One decoding step over a paged cache that already holds the newest token's rows (seg_kv_paged_append):
+ * q [B,Hq,D] bf16; out [B,Hq,D] bf16 or fp32 (cfg->out_fp32); lse [B,Hq].  A query head that sees no row has
+ * zeros and -infinity.  max_rows (host, <= max_pages * page_rows): the most rows of a head; it sizes the launch
+ * and the workspace, and of a head that holds more only the first max_rows are seen.  accumulate = 1: pages->mass
+ * of every row of a PAST head grows by the weight that the row has for this token, summed over the query heads
+ * of its group (at least one PAST head; EINVAL without mass).  At most 128 query heads per KV head.
+ * workspace: device, >= ..._workspace_bytes() (0: invalid arguments), 256-byte aligned, overwritten: calls that
+ * may overlap need one each. */
+size_t seg_attn_decode_paged_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
+                                             int64_t max_rows, int32_t accumulate);
+segattn_status seg_attn_decode_paged(const segattn_config *cfg, const segattn_pages *pages, const void *q,
+                                     const int32_t *rows, int64_t max_rows, int32_t accumulate, void *out,
+                                     float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Eviction by accumulated attention weight, in place.  Of every PAST head that holds more than keep_rows rows
+ * exactly keep_rows stay: those at the keep_recent newest positions (above the largest position held minus
+ * keep_recent), those at positions below keep_first, and of the others the ones with the largest mass (a
+ * negative or NaN mass counts as 0; among equals the lower row stays).  Rows that stay and lie at row keep_rows or behind
+ * move, in order, into the rows below that became free, also in order, with their scales, mass and position; no
+ * other row changes place.  rows_out[b,h] = min(rows[b,h], keep_rows) for a PAST head and rows[b,h] for the others
+ * (rows_out may be rows); pages that hold no row any more are the caller's again.  keep_recent + keep_first <=
+ * keep_rows.  pages->mass and pages->pos are required, and at least one PAST head.  max_rows as above.
+ * A row without a page counts as mass 0.  workspace as above. */
+size_t seg_kv_paged_evict_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
+                                          int64_t max_rows, int64_t keep_rows);
+segattn_status seg_kv_paged_evict(const segattn_config *cfg, const segattn_pages *pages, const int32_t *rows,
+                                  int64_t max_rows, int64_t keep_rows, int64_t keep_recent,
+                                  int64_t keep_first, int32_t *rows_out, void *workspace,
+                                  size_t workspace_bytes, void *stream);
 
 /* ---- misc ------------------------------------------------------------------------------- */
 /* Diagnostic for benchmarks: stream `bytes` of device memory at buf (16-byte aligned) with one of

@@ -13,6 +13,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libsegattn.so")
 SEGATTN_OK, SEGATTN_EINVAL, SEGATTN_ECAPACITY, SEGATTN_ESTATE, SEGATTN_EHIP, SEGATTN_ESCRATCH = range(6)
 SEGATTN_BWD_STATIC_SCRATCH_BYTES = 8 << 20
 SEGATTN_SEG, SEGATTN_TAIL, SEGATTN_PAST = 0, 1, 2
+SEGATTN_ROPE_PLAIN, SEGATTN_ROPE_LINEAR, SEGATTN_ROPE_BY_ROTATIONS, SEGATTN_ROPE_BY_INDEX = range(4)
+SEGATTN_PAGES_BF16, SEGATTN_PAGES_E4M3 = 0, 1
 
 
 class SegattnError(RuntimeError):
@@ -37,6 +39,21 @@ class segattn_retrieval(ctypes.Structure):
                 ("n_anchors", ctypes.c_int32), ("win_before", ctypes.c_int32), ("win_after", ctypes.c_int32)]
 
 
+class segattn_rope(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("factor", ctypes.c_double), ("trained_len", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("magnitude", ctypes.c_double),
+                ("inv_freq", ctypes.POINTER(ctypes.c_double))]
+
+
+class segattn_pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("type", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("per_head", ctypes.c_int32),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("mass", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p), ("table", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -51,6 +68,7 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         cfgp = ctypes.POINTER(segattn_config)
+        ropep, pagesp = ctypes.POINTER(segattn_rope), ctypes.POINTER(segattn_pages)
         sig = {
             "segattn_cache_bytes": (sz, [cfgp]),
             "segattn_create": (ctypes.c_int, [cfgp, vp, sz, ctypes.POINTER(vp)]),
@@ -83,6 +101,12 @@ def lib() -> ctypes.CDLL:
             "segattn_cache_span": (ctypes.c_int, [vp, i32, i32, ctypes.POINTER(sz), ctypes.POINTER(sz), ctypes.POINTER(i64)]),
             "segattn_resident_bytes": (sz, [vp]),
             "seg_attn_decode": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp]),
+            "seg_rope_rotate": (ctypes.c_int, [cfgp, ropep, vp, i64, vp, i64, i64, vp, vp, i32, i32, vp, i64, vp, i64, vp]),
+            "seg_kv_paged_append": (ctypes.c_int, [cfgp, pagesp, ropep, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp]),
+            "seg_attn_decode_paged_workspace_bytes": (sz, [cfgp, pagesp, i64, i32]),
+            "seg_attn_decode_paged": (ctypes.c_int, [cfgp, pagesp, vp, vp, i64, i32, vp, vp, vp, sz, vp]),
+            "seg_kv_paged_evict_workspace_bytes": (sz, [cfgp, pagesp, i64, i64]),
+            "seg_kv_paged_evict": (ctypes.c_int, [cfgp, pagesp, vp, i64, i64, i64, i64, vp, vp, sz, vp]),
             "segattn_bandwidth_probe": (ctypes.c_int, [vp, sz, i32, vp, vp]),
             "segattn_clock_probe": (ctypes.c_int, [ctypes.c_uint32, vp, ctypes.POINTER(i32), vp]),
             "segattn_mfma_probe": (ctypes.c_int, [i32, i32, vp, ctypes.POINTER(i64), vp]),
@@ -100,7 +124,8 @@ def lib() -> ctypes.CDLL:
 EXPORTS = ("segattn_cache_bytes", "segattn_create", "segattn_destroy", "segattn_reset", "seg_attn_fwd",
            "seg_attn_fwd_seq", "seg_attn_fwd_varlen", "segattn_layer_policy", "seg_rope_apply", "seg_attn_bwd_workspace_bytes", "seg_attn_bwd_seq", "seg_attn_bwd_seq_static", "seg_attn_bwd_varlen_workspace_bytes", "seg_attn_bwd_varlen", "seg_kv_commit", "seg_kv_commit_seq", "seg_kv_past_append", "seg_kv_past_select", "seg_kv_retrieve_workspace_bytes", "seg_kv_retrieve", "seg_kv_retrieve_seq_workspace_bytes", "seg_kv_retrieve_seq", "seg_attn_fwd_seq_retrieved_workspace_bytes", "seg_attn_fwd_seq_retrieved", "seg_kv_past_evict", "seg_kv_past_keep_recent",
            "seg_kv_lengths", "seg_kv_set_lengths", "segattn_cache_span", "segattn_resident_bytes",
-           "seg_attn_decode", "segattn_bandwidth_probe", "segattn_clock_probe", "segattn_mfma_probe", "segattn_strerror", "segattn_version")
+           "seg_attn_decode", "seg_rope_rotate", "seg_kv_paged_append", "seg_attn_decode_paged_workspace_bytes", "seg_attn_decode_paged",
+           "seg_kv_paged_evict_workspace_bytes", "seg_kv_paged_evict", "segattn_bandwidth_probe", "segattn_clock_probe", "segattn_mfma_probe", "segattn_strerror", "segattn_version")
 
 
 def _ptr(x) -> Optional[int]:
@@ -325,3 +350,61 @@ def segattn_mfma_probe(iterations: int, sink, stream=None, operands: int = 0) ->
 def seg_attn_decode(ctx: int, q, k_new, v_new, out, lse, stream=None) -> None:
     _check(lib().seg_attn_decode(ctx, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse), _ptr(stream)),
            "seg_attn_decode")
+
+
+def make_rope(*, theta: float, rotary_dim: int = 0, interleaved: bool = False, scaling: int = SEGATTN_ROPE_PLAIN,
+              factor: float = 1.0, trained_len: float = 0.0, low: float = 0.0, high: float = 0.0, magnitude: float = 0.0,
+              inv_freq: Optional[Sequence[float]] = None) -> segattn_rope:
+    freq = (ctypes.c_double * len(inv_freq))(*[float(x) for x in inv_freq]) if inv_freq is not None else None
+    rope = segattn_rope(theta, rotary_dim, int(interleaved), scaling, factor, trained_len, low, high, magnitude,
+                        ctypes.cast(freq, ctypes.POINTER(ctypes.c_double)) if freq is not None else None)
+    rope._inv_freq_keepalive = freq
+    return rope
+
+
+def seg_rope_rotate(cfg: segattn_config, rope: segattn_rope, q, k, rows: int, q_out, k_out, *, pos0=None, pos=None,
+                    inverse: bool = False, fp32: bool = False, q_stride: int = 0, k_stride: int = 0,
+                    q_out_stride: int = 0, k_out_stride: int = 0, stream=None) -> None:
+    _check(lib().seg_rope_rotate(ctypes.byref(cfg), ctypes.byref(rope), _ptr(q), q_stride, _ptr(k), k_stride, rows,
+                                 _ptr(pos0), _ptr(pos), int(inverse), int(fp32), _ptr(q_out), q_out_stride, _ptr(k_out),
+                                 k_out_stride, _ptr(stream)), "seg_rope_rotate")
+
+
+def make_pages(*, k, v, table, max_pages: int, page_rows: int, n_pages: int, per_head: bool = False, e4m3: bool = False,
+               page_stride: int = 0, head_stride: int = 0, row_stride: int = 0, k_scale=None, v_scale=None, mass=None,
+               pos=None) -> segattn_pages:
+    pages = segattn_pages(_ptr(k), _ptr(v), SEGATTN_PAGES_E4M3 if e4m3 else SEGATTN_PAGES_BF16, page_rows, n_pages,
+                          max_pages, int(per_head), page_stride, head_stride, row_stride, _ptr(k_scale), _ptr(v_scale),
+                          _ptr(mass), _ptr(pos), _ptr(table))
+    pages._keepalive = (k, v, table, k_scale, v_scale, mass, pos)
+    return pages
+
+
+def seg_kv_paged_append(cfg: segattn_config, pages: segattn_pages, rope: Optional[segattn_rope], q, k, v, cu_seqlens,
+                        total: int, max_seqlen: int, pos0, rows, q_out, rows_out, stream=None) -> None:
+    _check(lib().seg_kv_paged_append(ctypes.byref(cfg), ctypes.byref(pages), ctypes.byref(rope) if rope is not None else None,
+                                     _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), total, max_seqlen, _ptr(pos0), _ptr(rows),
+                                     _ptr(q_out), _ptr(rows_out), _ptr(stream)), "seg_kv_paged_append")
+
+
+def seg_attn_decode_paged_workspace_bytes(cfg: segattn_config, pages: segattn_pages, max_rows: int,
+                                          accumulate: bool = False) -> int:
+    return int(lib().seg_attn_decode_paged_workspace_bytes(ctypes.byref(cfg), ctypes.byref(pages), max_rows, int(accumulate)))
+
+
+def seg_attn_decode_paged(cfg: segattn_config, pages: segattn_pages, q, rows, max_rows: int, out, lse, workspace,
+                          workspace_bytes: int, accumulate: bool = False, stream=None) -> None:
+    _check(lib().seg_attn_decode_paged(ctypes.byref(cfg), ctypes.byref(pages), _ptr(q), _ptr(rows), max_rows, int(accumulate),
+                                       _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes, _ptr(stream)),
+           "seg_attn_decode_paged")
+
+
+def seg_kv_paged_evict_workspace_bytes(cfg: segattn_config, pages: segattn_pages, max_rows: int, keep_rows: int) -> int:
+    return int(lib().seg_kv_paged_evict_workspace_bytes(ctypes.byref(cfg), ctypes.byref(pages), max_rows, keep_rows))
+
+
+def seg_kv_paged_evict(cfg: segattn_config, pages: segattn_pages, rows, max_rows: int, keep_rows: int, keep_recent: int,
+                       keep_first: int, rows_out, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib().seg_kv_paged_evict(ctypes.byref(cfg), ctypes.byref(pages), _ptr(rows), max_rows, keep_rows, keep_recent,
+                                    keep_first, _ptr(rows_out), _ptr(workspace), workspace_bytes, _ptr(stream)),
+           "seg_kv_paged_evict")

@@ -20,7 +20,9 @@ constexpr unsigned long long kAlign = 256;
 
 unsigned long long align_up(unsigned long long x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-bool build_problem(const segattn_config *cfg, bool need_cache, Problem &p) {
+}  // namespace
+
+bool segattn::build_problem(const segattn_config *cfg, bool need_cache, Problem &p) {
   if (!cfg || !cfg->kv_policy) return false;
   if (cfg->batch < 1 || cfg->n_kv_heads < 1 || cfg->n_kv_heads > kMaxKvHeads) return false;
   if (cfg->n_q_heads < 1 || cfg->n_q_heads % cfg->n_kv_heads) return false;
@@ -68,6 +70,8 @@ bool build_problem(const segattn_config *cfg, bool need_cache, Problem &p) {
   }
   return true;
 }
+
+namespace {
 
 bool build_geom(const segattn_config *cfg, const Problem &p, CacheGeom &g, unsigned long long &total) {
   memset(&g, 0, sizeof(g));

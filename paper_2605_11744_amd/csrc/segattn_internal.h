@@ -524,6 +524,10 @@ __device__ inline long long ws_slot_base(const Problem &p, const CacheGeom &g, i
 }
 
 
+// The checked configuration; false where it is not valid.  need_cache: past_capacity and the retrieval
+// mode count too.
+bool build_problem(const segattn_config *cfg, bool need_cache, Problem &p);
+
 // ---- launchers (defined in the .hip files) ------------------------------------------------
 int device_cus();  // compute units of the device, asked once
 // The form of a prefill launch: heads and waves of a workgroup, the key-split kernel or the pipelined one, prefixes cut into

@@ -1,0 +1,536 @@
+// seg_attn_decode_paged: attention of one new token per sequence over a paged cache.
+//
+// The g query heads of a KV head are the columns of 16-column matrix operands (16 per pass).  Per tile of
+// 32 key rows a wave forms
+//   S^T[key][head] = K . Q^T            v_mfma_f32_16x16x32_bf16, A = K rows, B = Q^T (registers)
+//   P = exp2((S^T - m) c)               running maximum m and sum l per head (lane = head), in fp32
+//   O^T[d][head] += V^T . P^T           A = V^T via ds_read_b64_tr_b16, B = P from the S^T registers
+// P enters the product as a bf16 and the bf16 of what that leaves (2^-17 of a weight is lost): the products are
+// idle beside the memory, and the output keeps the accuracy of the type it is rounded to.
+//
+// The work is bound by memory: every seen row is read once per KV head.  The windows of all (sequence, KV
+// head) pairs are cut into slices of whole tiles, found by the kernel itself from the row counts on the
+// device, so a captured launch serves a cache that grows.  At the end of every window a workgroup writes one
+// partial (acc[D], m, l) per query head; a second launch merges them and, where the cache keeps the weight
+// of its rows, turns the stored scores into weights and adds them up.
+#include "segattn_paged.h"
+
+namespace segattn {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+#define LDS_AS __attribute__((address_space(3)))
+
+constexpr int kPagedHeads = 16;  // query heads per pass
+constexpr int kPagedWaves = 4;
+
+// Rows [first, n) of a window that the newest token (row n - 1) sees.
+__device__ inline void paged_window(const PagedDecodeArgs &a, int w, int &first, int &n) {
+  n = rows_held(a.rows, w, a.max_rows);
+  const int h = w - fast_div(w, a.n_kv) * a.Hkv;
+  first = 0;
+  if (!in_set(a.heads.past, h)) {
+    const int start = fast_div(n > 0 ? n - 1 : 0, a.seg) * (int)a.seg.d;
+    first = in_set(a.heads.tail, h) ? (start > a.tail ? start - a.tail : 0) : start;
+  }
+}
+__device__ inline int paged_tiles(const PagedDecodeArgs &a, int w) {
+  int first, n;
+  paged_window(a, w, first, n);
+  return (n + kPagedTile - 1) / kPagedTile - first / kPagedTile;  // 0 for n = 0
+}
+
+// This workgroup's slice: tiles [tile, tile + count) counted from window w's first one; a count that goes beyond the
+// window goes on in the next ones (not in the first form).  Every slice is a multiple of one tile per wave.
+struct PagedSlice {
+  int w, tile, count;
+  bool by_window;
+};
+__device__ inline PagedSlice paged_slice(const PagedDecodeArgs &a, int wgs) {
+  const int lane = threadIdx.x & 63, me = blockIdx.x;
+  constexpr int kLeast = kPagedWaves;
+  auto whole = [](int tiles) { return (tiles + kPagedWaves - 1) / kPagedWaves * kPagedWaves; };
+  PagedSlice s{-1, 0, 0, true};
+  if (a.n_windows <= kPagedLaneWindows) {
+    // Few windows: each is cut by itself, into slices as long as the grid needs them, a lane per window.
+    const int tiles = lane < a.n_windows ? paged_tiles(a, lane) : 0;
+    int count = kLeast;
+    if (!a.fits) {
+      int total = tiles;
+#pragma unroll
+      for (int sh = 1; sh < 64; sh <<= 1) total += __shfl_xor(total, sh);
+      const int spare = wgs - a.n_windows;  // sum of ceil(t / c) <= total / c + windows <= wgs
+      count = whole((total + spare - 1) / spare);
+      count = count < kLeast ? kLeast : count;
+    }
+    const int mine = (tiles + count - 1) / count;
+    int incl = mine;
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) {
+      const int up = __shfl_up(incl, sh);
+      if (lane >= sh) incl += up;
+    }
+    const unsigned long long reach = __builtin_amdgcn_ballot_w64(incl > me);
+    if (reach == 0) return s;
+    s.w = (int)__builtin_ctzll(reach);
+    s.tile = (me - __builtin_amdgcn_readlane(incl - mine, s.w)) * count;
+    s.count = count;
+    return s;
+  }
+  // Many windows: all tiles end to end, cut evenly.  A thread adds up a run of consecutive windows, every wave scans
+  // the 256 sums, four a lane, and walks the run that holds the slice's first tile.
+  __shared__ __attribute__((aligned(16))) int sm_run[256];
+  const int tid = threadIdx.x, run = (a.n_windows + 255) / 256;
+  int sum = 0;
+  for (int j = 0; j < run; ++j)
+    if (tid * run + j < a.n_windows) sum += paged_tiles(a, tid * run + j);
+  sm_run[tid] = sum;
+  __syncthreads();
+  int part[4], incl = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    part[j] = sm_run[4 * lane + j];
+    incl += part[j];
+  }
+  const int mine = incl;
+#pragma unroll
+  for (int sh = 1; sh < 64; sh <<= 1) {
+    const int up = __shfl_up(incl, sh);
+    if (lane >= sh) incl += up;
+  }
+  const int total = __builtin_amdgcn_readlane(incl, 63);
+  int count = whole((total + wgs - 1) / wgs);
+  count = count < kLeast ? kLeast : count;
+  if (total == 0 || me > (total - 1) / count) return s;
+  const int start = me * count;  // < total
+  const int L = (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(incl > start));
+  int before = __builtin_amdgcn_readlane(incl - mine, L), t = 4 * L;
+#pragma unroll
+  for (int j = 0; j < 3; ++j) {
+    const int n = __builtin_amdgcn_readlane(part[j], L);
+    if (t == 4 * L + j && before + n <= start) {
+      before += n;
+      ++t;
+    }
+  }
+  int w = t * run;
+  for (int j = 0; j + 1 < run; ++j) {
+    const int n = paged_tiles(a, w);
+    if (before + n > start) break;
+    before += n;
+    ++w;
+  }
+  s.w = __builtin_amdgcn_readfirstlane(w);
+  s.tile = __builtin_amdgcn_readfirstlane(start - before);
+  s.count = count;
+  s.by_window = false;
+  return s;
+}
+
+__device__ inline float over_quads(float x, bool sum) {  // over the four lanes of a column
+  const float y = __shfl_xor(x, 16);
+  x = sum ? x + y : fmaxf(x, y);
+  const float z = __shfl_xor(x, 32);
+  return sum ? x + z : fmaxf(x, z);
+}
+
+// kInPage: page_rows is a multiple of the tile, so a tile lies in one page; otherwise every row asks the table.
+template <int D, bool kE4m3, bool kInPage>
+__global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedDecodeArgs a) {
+  constexpr int NK = D / 32, NB = D / 16;
+  constexpr int kRow = 2 * D, kTileBytes = kPagedTile * kRow;  // of a tile in LDS, bf16
+  constexpr int kPieces = (kE4m3 ? D : 2 * D) / 16;            // 16-byte pieces of a row in memory
+  constexpr int RPL = 64 / kPieces, NL = kPagedTile / RPL;     // rows per wave load, loads per tile and tensor
+  // XOR on the number of a row's 16-byte chunk: 16 rows read at one chunk (K), or 8 rows at two (V), meet every bank once
+  auto swz_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
+  auto swz_v = [](int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
+
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int quad = lane >> 4, col = lane & 15;
+  const float c = a.scale_log2e;
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[kPagedWaves][2 * kTileBytes];
+  constexpr int MS = D + 4;  // floats per head of the merge area
+  static_assert(kPagedWaves * 2 * kTileBytes >= (int)sizeof(float) * kPagedWaves * kPagedHeads * MS, "merge area fits the tiles");
+
+  const PagedSlice slice = paged_slice(a, gridDim.x);
+  if (slice.w < 0) return;
+  const int pass = blockIdx.y, live = min(kPagedHeads, a.g - pass * kPagedHeads);
+  unsigned char *tile = tiles[wave];
+  int koff[2][NK], voff[2][NB];
+#pragma unroll
+  for (int h2 = 0; h2 < 2; ++h2) {
+    const int krow = 16 * h2 + col, vrow = 16 * h2 + 4 * quad + (col >> 2);
+#pragma unroll
+    for (int kc = 0; kc < NK; ++kc) koff[h2][kc] = krow * kRow + (((4 * kc + quad) ^ swz_k(krow)) << 4);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+      voff[h2][nb] = kTileBytes + vrow * kRow + (((2 * nb + ((col & 3) >> 1)) ^ swz_v(vrow)) << 4) + 8 * (col & 1);
+  }
+
+  int left = slice.count;
+  for (int w = slice.w, tile0 = slice.tile; left > 0 && w < a.n_windows; ++w, tile0 = 0) {
+    int first, n;
+    paged_window(a, w, first, n);
+    first = __builtin_amdgcn_readfirstlane(first);
+    n = __builtin_amdgcn_readfirstlane(n);
+    const int base = first / kPagedTile, all = (n + kPagedTile - 1) / kPagedTile - base;
+    const int t_begin = base + tile0, t_end = base + min(all, tile0 + left);
+    if (t_end <= t_begin) continue;
+    left = slice.by_window ? 0 : left - (t_end - t_begin);
+    const int b = fast_div(w, a.n_kv), h = w - b * a.Hkv;
+    const int head0 = h * a.g + pass * kPagedHeads;
+    const int *table = table_of(a.c, a.Hkv, b, h);
+    const int hh = a.c.per_head ? 0 : h;
+
+    bf16x8 Q[NK];  // column col = head head0 + col, zero beyond the live ones
+    {
+      const unsigned short *q = a.q + ((long long)b * a.Hq + head0 + (col < live ? col : 0)) * D + 8 * quad;
+#pragma unroll
+      for (int kc = 0; kc < NK; ++kc) {
+        u32x4 x = *(const u32x4 *)(q + 32 * kc);
+        if (col >= live) x = u32x4{0u, 0u, 0u, 0u};
+        Q[kc] = __builtin_bit_cast(bf16x8, x);
+      }
+    }
+    f32x4 O[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) O[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
+
+    float *scores = nullptr;
+    if (a.scores && in_set(a.heads.past, h) && col < live)
+      scores = a.scores + ((long long)(b * a.n_past + set_before(a.heads.past, h)) * a.g + pass * kPagedHeads + col) * a.score_rows;
+
+    u32x4 nk[NL], nv[NL];     // the wave's next tile, in flight
+    int n_scale = 0;          // scale byte of row lane % 32: keys in the lower half of the wave, values in the upper
+    unsigned n_valid = 0;     // rows of it that count
+    int entry = 0, entry_row = 0;  // the table's entry for the tile after that (kInPage), or for this lane's row of it
+    auto ask = [&](int t) __attribute__((always_inline)) {
+      if constexpr (kInPage) {
+        entry = table[fast_div(t * kPagedTile, a.c.page_rows)];
+      } else {
+        int r = t * kPagedTile + (lane & 31);
+        r = r < n ? r : n - 1;
+        const int i = fast_div(r, a.c.page_rows);
+        entry = table[i];
+        entry_row = r - i * (int)a.c.page_rows.d;
+      }
+    };
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+      const int r0 = t * kPagedTile;
+      unsigned valid = ~0u;
+      if (r0 < first) valid &= ~0u << (first - r0);
+      if (r0 + kPagedTile > n) valid &= (1u << (n - r0)) - 1u;
+      const bool named = (unsigned)entry < (unsigned)a.c.n_pages;
+      const int page = named ? entry : 0;  // rows without a page: some row that exists, with weight 0
+      if constexpr (kInPage) {
+        const int pg = __builtin_amdgcn_readfirstlane(page);
+        if (!__builtin_amdgcn_readfirstlane(named)) valid = 0;
+        const int in_page = r0 - fast_div(r0, a.c.page_rows) * (int)a.c.page_rows.d;
+        const long long at = pg * a.c.page_bytes + hh * a.c.head_bytes + in_page * a.c.row_bytes;
+        const unsigned mine = (unsigned)(lane / kPieces) * (unsigned)a.c.row_bytes + (lane % kPieces) * 16;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const long long step = at + i * (RPL * a.c.row_bytes);
+          nk[i] = __builtin_nontemporal_load((const u32x4 *)(a.c.k + step + mine));
+          nv[i] = __builtin_nontemporal_load((const u32x4 *)(a.c.v + step + mine));
+        }
+        if constexpr (kE4m3) {
+          const long long place = ((long long)pg * a.c.heads + hh) * a.c.page_rows.d + in_page + (lane & 31);
+          n_scale = (lane < 32 ? a.c.k_scale : a.c.v_scale)[place];
+        }
+      } else {
+        valid &= (unsigned)__builtin_amdgcn_ballot_w64(named);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int r = RPL * i + lane / kPieces;
+          const long long at = __shfl(page, r) * a.c.page_bytes + hh * a.c.head_bytes + __shfl(entry_row, r) * a.c.row_bytes + (lane % kPieces) * 16;
+          nk[i] = __builtin_nontemporal_load((const u32x4 *)(a.c.k + at));
+          nv[i] = __builtin_nontemporal_load((const u32x4 *)(a.c.v + at));
+        }
+        if constexpr (kE4m3) {
+          const long long place = ((long long)page * a.c.heads + hh) * a.c.page_rows.d + entry_row;
+          n_scale = (lane < 32 ? a.c.k_scale : a.c.v_scale)[place];
+        }
+      }
+      n_valid = valid;
+    };
+    // A tile into LDS; rows that do not count as zeros (a weight of zero times NaN would be NaN).
+    auto stage = [&](unsigned valid) __attribute__((always_inline)) {
+      const bool whole = valid == ~0u;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int r = RPL * i + lane / kPieces, piece = lane % kPieces;
+        u32x4 xk = nk[i], xv = nv[i];
+        if (!whole && !((valid >> r) & 1)) xk = xv = u32x4{0u, 0u, 0u, 0u};
+        if constexpr (!kE4m3) {
+          *(u32x4 *)(tile + r * kRow + ((piece ^ swz_k(r)) << 4)) = xk;
+          *(u32x4 *)(tile + kTileBytes + r * kRow + ((piece ^ swz_v(r)) << 4)) = xv;
+        } else {
+          // a scale is a power of two and e4m3 has four significant bits: the bf16 is exact
+          const float sk = __uint_as_float((unsigned)__shfl(n_scale, r) << 23), sv = __uint_as_float((unsigned)__shfl(n_scale, r + 32) << 23);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            bf16x2 yk[4], yv[4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              yk[2 * e] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xk[2 * half + e], sk, false);
+              yk[2 * e + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xk[2 * half + e], sk, true);
+              yv[2 * e] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[2 * half + e], sv, false);
+              yv[2 * e + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[2 * half + e], sv, true);
+            }
+            const int chunk = 2 * piece + half;
+            *(u32x4 *)(tile + r * kRow + ((chunk ^ swz_k(r)) << 4)) = __builtin_bit_cast(u32x4, yk);
+            *(u32x4 *)(tile + kTileBytes + r * kRow + ((chunk ^ swz_v(r)) << 4)) = __builtin_bit_cast(u32x4, yv);
+          }
+        }
+      }
+    };
+
+    int t = t_begin + wave;
+    if (t < t_end) {
+      ask(t);
+      fetch(t);
+      if (t + kPagedWaves < t_end) ask(t + kPagedWaves);
+    }
+    for (; t < t_end; t += kPagedWaves) {
+      const unsigned valid = n_valid;
+      stage(valid);
+      if (t + kPagedWaves < t_end) {
+        fetch(t + kPagedWaves);
+        if (t + 2 * kPagedWaves < t_end) ask(t + 2 * kPagedWaves);
+      }
+      f32x4 S[2];
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2) {
+        S[h2] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kc = 0; kc < NK; ++kc)
+          S[h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)(tile + koff[h2][kc]), Q[kc], S[h2], 0, 0, 0);
+      }
+      // register r of S[h2] is key 16 h2 + 4 quad + r
+      if (valid != ~0u) {
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!((valid >> (16 * h2 + 4 * quad + r)) & 1)) S[h2][r] = -INFINITY;
+      }
+      if (scores) {
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) *(f32x4 *)(scores + t * kPagedTile + 16 * h2 + 4 * quad) = S[h2];
+      }
+      float mx = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
+      mx = over_quads(mx, false);
+      const float m_new = fmaxf(m_run, mx);
+      const float ref = m_new == -INFINITY ? 0.f : m_new;  // no row yet
+      const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * c);
+      m_run = m_new;
+      bf16x8 P, P_rest;
+      float sum = 0.f;
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float e = __builtin_amdgcn_exp2f((S[h2][r] - ref) * c);
+          sum += e;
+          P[4 * h2 + r] = (__bf16)e;
+          P_rest[4 * h2 + r] = (__bf16)(e - (float)P[4 * h2 + r]);
+        }
+      l_run = l_run * alpha + sum;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        O[nb] *= alpha;
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[0][nb]));
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[1][nb]));
+        const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        O[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, P, O[nb], 0, 0, 0);
+        O[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, P_rest, O[nb], 0, 0, 0);
+      }
+    }
+    l_run = over_quads(l_run, true);
+
+    // ---- this window's partial: the waves meet in LDS (over the tiles: everyone is done)
+    __syncthreads();
+    float *mg = (float *)&tiles[0][0];  // [wave][head][MS]
+    if (col < live) {
+      float *dst = mg + (wave * kPagedHeads + col) * MS;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(dst + 16 * nb + 4 * quad) = O[nb];
+      if (quad == 0) {
+        dst[D] = m_run;
+        dst[D + 1] = l_run;
+      }
+    }
+    __syncthreads();
+    const long long slot = blockIdx.x + (slice.by_window ? 0 : w);
+    for (int i = tid; i < live * (D / 4); i += 64 * kPagedWaves) {
+      const int head = i / (D / 4), d = (i % (D / 4)) * 4;
+      float top = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < kPagedWaves; ++x) top = fmaxf(top, mg[(x * kPagedHeads + head) * MS + D]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float l = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < kPagedWaves; ++x) {
+        const float *src = mg + (x * kPagedHeads + head) * MS;
+        // 0 for a wave without rows; one whose scores are all NaN has no maximum either, and its NaN sums stay NaN
+        const float wgt = __builtin_amdgcn_exp2f((src[D] - ref) * c);
+        l += src[D + 1] * wgt;
+        const f32x4 part = *(const f32x4 *)(src + d);
+        o += part * wgt;
+      }
+      float *dst = a.slots + (slot * a.g + pass * kPagedHeads + head) * ws_slot_floats(D);
+      *(f32x4 *)(dst + d) = o;
+      if (d == 0) *(float2 *)(dst + D) = float2{top, l};
+    }
+    if (tid == 0 && pass == 0) {
+      if (tile0 == 0) a.pieces[w].x = (int)slot;
+      if (t_end == base + all) a.pieces[w].y = (int)slot;
+    }
+    __syncthreads();  // the merge area is tile space again
+  }
+}
+
+// Maximum and sum of one head of a window over its partials, in the wave that asks (lanes take the partials in turn).
+__device__ inline void joined_sum(const float *ml, long long stride, int count, float c, float &top, float &l) {
+  const int lane = threadIdx.x & 63;
+  top = -INFINITY;
+  l = 0.f;
+  for (int s = lane; s < count; s += 64) {
+    const float2 x = *(const float2 *)(ml + s * stride);
+    const float m_new = fmaxf(top, x.x), ref = m_new == -INFINITY ? 0.f : m_new;
+    l = l * __builtin_amdgcn_exp2f((top - ref) * c) + x.y * __builtin_amdgcn_exp2f((x.x - ref) * c);
+    top = m_new;
+  }
+#pragma unroll
+  for (int sh = 1; sh < 64; sh <<= 1) {
+    const float m2 = __shfl_xor(top, sh), l2 = __shfl_xor(l, sh);
+    const float m_new = fmaxf(top, m2), ref = m_new == -INFINITY ? 0.f : m_new;
+    l = l * __builtin_amdgcn_exp2f((top - ref) * c) + l2 * __builtin_amdgcn_exp2f((m2 - ref) * c);
+    top = m_new;
+  }
+}
+
+constexpr int kMassRows = 1024;  // rows a workgroup adds the weights of
+
+// Workgroups 0 .. B Hq - 1: merge of one query head's partials.  The others: weights of kMassRows rows of one PAST
+// head's window, from the scores that the first launch left.
+template <int D>
+__global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecodeArgs a, const int mass_chunks) {
+  constexpr int SF = D + kWsTailFloats, DPL = D / 64;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const float c = a.scale_log2e;
+  const int heads = a.B * a.Hq;
+  if ((int)blockIdx.x < heads) {
+    const int b = blockIdx.x / a.Hq, head = blockIdx.x - b * a.Hq, w = b * a.Hkv + head / a.g;
+    __shared__ float sm_m[4], sm_l[4], sm_o[4][D];
+    const bool some = paged_tiles(a, w) > 0;
+    const int2 piece = some ? a.pieces[w] : int2{0, -1};
+    const float *ws = a.slots + ((long long)piece.x * a.g + head % a.g) * SF;
+    const int count = piece.y - piece.x + 1;
+    float top = -INFINITY, l = 0.f, o[DPL];
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) o[e] = 0.f;
+    for (int s = wave; s < count; s += 4) {
+      const float *src = ws + (long long)s * a.g * SF;
+      const float2 ml = *(const float2 *)(src + D);
+      const float m_new = fmaxf(top, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float keep = __builtin_amdgcn_exp2f((top - ref) * c), wgt = __builtin_amdgcn_exp2f((ml.x - ref) * c);
+      top = m_new;
+      l = l * keep + ml.y * wgt;
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) o[e] = o[e] * keep + src[lane * DPL + e] * wgt;
+    }
+    if (lane == 0) {
+      sm_m[wave] = top;
+      sm_l[wave] = l;
+    }
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) sm_o[wave][lane * DPL + e] = o[e];
+    __syncthreads();
+    if (tid >= D) return;
+    top = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+    const float ref = top == -INFINITY ? 0.f : top;
+    l = 0.f;
+    float od = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float wgt = __builtin_amdgcn_exp2f((sm_m[x] - ref) * c);
+      l += sm_l[x] * wgt;
+      od += sm_o[x][tid] * wgt;
+    }
+    const float r = l == 0.f ? 0.f : od / l;  // no row seen: zeros, and the logarithm of nothing
+    const long long at = ((long long)b * a.Hq + head) * D + tid;
+    if (a.out_fp32) ((float *)a.out)[at] = r;
+    else ((__bf16 *)a.out)[at] = (__bf16)r;
+    if (tid == 0) a.lse[(long long)b * a.Hq + head] = l == 0.f ? -INFINITY : ref * a.scale + logf(l);
+    return;
+  }
+  const int i = blockIdx.x - heads, win = i / mass_chunks, chunk = i - win * mass_chunks;
+  const int b = win / a.n_past;
+  int h = 0;  // the (win % n_past)-th PAST head
+  for (int k = win - b * a.n_past; h < a.Hkv; ++h)
+    if (in_set(a.heads.past, h) && k-- == 0) break;
+  const int w = b * a.Hkv + h, n = rows_held(a.rows, w, a.max_rows);
+  if (chunk * kMassRows >= n) return;
+  __shared__ float sm_top[kPagedMostGroup], sm_share[kPagedMostGroup];
+  const int2 piece = a.pieces[w];
+  for (int j = wave; j < a.g; j += 4) {
+    float top, l;
+    joined_sum(a.slots + ((long long)piece.x * a.g + j) * SF + D, (long long)a.g * SF, piece.y - piece.x + 1, c, top, l);
+    if (lane == 0) {
+      sm_top[j] = top == -INFINITY ? 0.f : top;
+      sm_share[j] = l == 0.f ? 0.f : 1.f / l;
+    }
+  }
+  __syncthreads();
+  const int *table = table_of(a.c, a.Hkv, b, h);
+  const float *scores = a.scores + (long long)win * a.g * a.score_rows;
+  for (int r = chunk * kMassRows + tid; r < n && r < (chunk + 1) * kMassRows; r += 256) {
+    int in_page;
+    const int page = page_of(a.c, table, r, in_page);
+    if (page < 0) continue;
+    float sum = 0.f;
+    for (int j = 0; j < a.g; ++j) sum += __builtin_amdgcn_exp2f((scores[j * a.score_rows + r] - sm_top[j]) * c) * sm_share[j];
+    a.c.mass[row_place(a.c, page, h, in_page)] += sum;
+  }
+}
+
+template <int D, bool kE4m3, bool kInPage>
+static hipError_t launch_split(PagedDecodeArgs a, hipStream_t st) {
+  static ResidentCount count;
+  const auto kern = paged_decode_split_kernel<D, kE4m3, kInPage>;
+  const int resident = count.get((const void *)kern, 256, 0);
+  if (resident == 0) return hipErrorUnknown;
+  long long grid = resident < kPagedMostWgs ? resident : kPagedMostWgs;
+  const long long tiles = (a.max_rows + kPagedTile - 1) / kPagedTile;
+  const long long slices = a.n_windows * ((tiles + kPagedWaves - 1) / kPagedWaves);  // at most, of the shortest length
+  a.fits = slices <= grid;
+  if (a.fits) grid = slices;
+  else if (a.n_windows <= kPagedLaneWindows && grid < 2 * a.n_windows) grid = 2 * a.n_windows;  // paged_slice needs spare ones
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid, (a.g + kPagedHeads - 1) / kPagedHeads), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+template <int D>
+static hipError_t launch_paged(const PagedDecodeArgs &a, hipStream_t st) {
+  const bool in_page = a.c.page_rows.d % kPagedTile == 0;
+  const hipError_t e = a.c.e4m3 ? (in_page ? launch_split<D, true, true>(a, st) : launch_split<D, true, false>(a, st))
+                                : (in_page ? launch_split<D, false, true>(a, st) : launch_split<D, false, false>(a, st));
+  if (e != hipSuccess) return e;
+  const int chunks = a.scores ? (a.max_rows + kMassRows - 1) / kMassRows : 0;
+  const long long grid = (long long)a.B * a.Hq + (long long)a.B * a.n_past * chunks;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(paged_decode_join_kernel<D>, dim3((unsigned)grid), dim3(256), 0, st, a, chunks);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_decode(const PagedDecodeArgs &a, hipStream_t st) {
+  return a.D == 128 ? launch_paged<128>(a, st) : launch_paged<64>(a, st);
+}
+
+}  // namespace segattn
