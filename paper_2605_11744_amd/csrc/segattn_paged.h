@@ -125,6 +125,8 @@ struct PagedEvictArgs {
   const int *rows;
   int *rows_out;
   int *moves;           // workspace: rows to move of every window
+  unsigned *keys;       // workspace: [window][key_rows], or nullptr where they fit the kernel's LDS
+  long long key_rows;
   int *lists;           // workspace: [window][2][most_moves]: freed places, then the rows that go there
   int B, Hkv, D;
   int max_rows, keep, recent, first, most_moves;
@@ -133,6 +135,7 @@ struct PagedEvictArgs {
 hipError_t launch_rotate(const RotateArgs &a, bool fp32, hipStream_t st);
 hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t st);
 hipError_t launch_paged_decode(const PagedDecodeArgs &a, hipStream_t st);
+bool evict_keys_held(long long max_rows);  // the keys of so many rows need no workspace
 hipError_t launch_paged_evict(const PagedEvictArgs &a, hipStream_t st);
 
 }  // namespace segattn

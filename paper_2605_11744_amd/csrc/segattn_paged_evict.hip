@@ -13,19 +13,29 @@
 
 namespace segattn {
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr unsigned kSureKey = 0xffffffffu;
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kHeldRows = 32 * kSelectThreads;  // rows whose keys fit the select kernel's LDS
+constexpr int kCopies = 16;       // of the histogram: neighbouring lanes count in different ones
+constexpr int kAtOnce = 8;        // rows of a lane that are under way together
 
-__device__ inline unsigned evict_key(const PagedEvictArgs &a, int newest, float mass, int pos) {
-  if ((long long)pos > (long long)newest - a.recent || (a.first > 0 && pos < a.first)) return kSureKey;
-  return mass > 0.f ? __float_as_uint(mass) : 0u;
-}
-
+// The select kernel walks over a window's keys seven times, so they are formed once (a key costs a look into the
+// table and two loads) and kept: in LDS (kHeld), or for longer windows in the workspace.  Wave x has a run of consecutive
+// rows, 64 at a time.  The histogram is kept kCopies times: weights share few exponents, and 64 lanes that count
+// the same byte in one word wait for each other.
+//
+// One compute unit works on a window, and a vector instruction more per 64 rows is 0.25 us more for 32768.  kInPage:
+// page_rows is a multiple of 64, so 64 rows lie in one page and are found with scalar instructions.
+template <bool kHeld, bool kInPage>
 __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const PagedEvictArgs a) {
   const int w = blockIdx.x, b = w / a.Hkv, h = w - b * a.Hkv;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  __shared__ int sm_hist[256], sm_part[kSelectWaves], sm_part2[kSelectWaves];
-  __shared__ int sm_pick[2];
+  extern __shared__ unsigned sm_keys[];
+  __shared__ int sm_hist[256 * kCopies];
+  __shared__ __attribute__((aligned(16))) int sm_part[kSelectWaves][4];
+  __shared__ int sm_pick[3];
   const int n = rows_held(a.rows, w, a.max_rows);
   __syncthreads();  // rows may be rows_out
   const bool evicts = in_set(a.heads.past, h) && n > a.keep;
@@ -34,50 +44,129 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
     if (!evicts) a.moves[w] = 0;
   }
   if (!evicts) return;
+  unsigned *keys;
+  if constexpr (kHeld) keys = sm_keys;
+  else keys = a.keys + (long long)w * a.key_rows;
   const int *table = table_of(a.c, a.Hkv, b, h);
-  int newest = -0x7fffffff - 1;
-  for (int r = tid; r < n; r += kSelectThreads) {
-    int in_page;
-    const int page = page_of(a.c, table, r, in_page);
-    if (page < 0) continue;
-    const int pos = a.c.pos[row_place(a.c, page, h, in_page)];
-    newest = pos > newest ? pos : newest;
+  const int run = (n + kSelectThreads - 1) / kSelectThreads * 64;
+  const int r0 = wave * run, r1 = r0 + run < n ? r0 + run : n;
+
+  // First the weights' bits, and the newest position; then the rows that stay for their position's sake.  A row without a
+  // page has weight 0 and no position.
+  constexpr int kNowhere = -0x7fffffff - 1;
+  int newest = kNowhere;
+  // Places of rows r + 64 i + lane, i < kAtOnce, or -1: of the first one of 64 (kInPage) or of the row.  kInPage: the
+  // table's entries for 64 steps of the wave are asked at once, one a lane.
+  long long place[kAtOnce];
+  int entry = -1;
+  auto ask = [&](int r) __attribute__((always_inline)) {
+    if constexpr (kInPage) {
+      if ((r - r0) % (64 * 64) == 0) {
+        int in_page;
+        const int row = r + 64 * lane;
+        entry = row < r1 ? page_of(a.c, table, row, in_page) : -1;
+      }
+    }
+  };
+  auto find = [&](int r) __attribute__((always_inline)) {
+    if constexpr (kInPage) {
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int row = r + 64 * i, page = __builtin_amdgcn_readlane(entry, ((row - r0) >> 6) & 63);
+        const int in_page = row - fast_div(row, a.c.page_rows) * (int)a.c.page_rows.d;
+        place[i] = page < 0 ? -1 : row_place(a.c, page, h, in_page);
+      }
+    } else {
+      int page[kAtOnce], in_page[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int row = r + 64 * i + lane;
+        page[i] = page_of(a.c, table, row < n ? row : n - 1, in_page[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) place[i] = page[i] < 0 ? -1 : row_place(a.c, page[i], h, in_page[i]);
+    }
+  };
+  const int beside = kInPage ? lane : 0;  // (a page has room for all 64 rows, also behind the last one)
+  for (int r = r0; r < r0 + run; r += 64 * kAtOnce) {
+    ask(r);
+    find(r);
+    int pos[kAtOnce];
+    float mass[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      pos[i] = (a.c.pos + (place[i] < 0 ? 0 : place[i]))[place[i] < 0 ? 0 : beside];
+      mass[i] = (a.c.mass + (place[i] < 0 ? 0 : place[i]))[place[i] < 0 ? 0 : beside];
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const bool held = place[i] >= 0 && r + 64 * i + lane < r1;
+      if (r + 64 * i < r0 + run) keys[r + 64 * i + lane] = held && mass[i] > 0.f ? __float_as_uint(mass[i]) : 0u;
+      if (held && pos[i] > newest) newest = pos[i];
+    }
   }
 #pragma unroll
   for (int sh = 1; sh < 64; sh <<= 1) {
     const int x = __shfl_xor(newest, sh);
     newest = x > newest ? x : newest;
   }
-  if (lane == 0) sm_part[wave] = newest;
+  if (lane == 0) sm_part[wave][0] = newest;
   __syncthreads();
-  newest = sm_part[0];
+  newest = sm_part[0][0];
 #pragma unroll
-  for (int x = 1; x < kSelectWaves; ++x) newest = sm_part[x] > newest ? sm_part[x] : newest;
-  __syncthreads();
-  auto key_of = [&](int r) __attribute__((always_inline)) {  // a row without a page: the lowest
-    int in_page;
-    const int page = page_of(a.c, table, r, in_page);
-    if (page < 0) return 0u;
-    const long long place = row_place(a.c, page, h, in_page);
-    return evict_key(a, newest, a.c.mass[place], a.c.pos[place]);
+  for (int x = 1; x < kSelectWaves; ++x) newest = sm_part[x][0] > newest ? sm_part[x][0] : newest;
+  // positions above newest - recent stay, as a bound that an int holds
+  const int above = (long long)newest - a.recent < kNowhere ? kNowhere : newest - a.recent;
+  const int from = a.first > 0 ? a.first : kNowhere;
+  for (int r = r0; r < r1; r += 64 * kAtOnce) {
+    if (run > 64 * 64) ask(r);
+    find(r);
+    int pos[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) pos[i] = (a.c.pos + (place[i] < 0 ? 0 : place[i]))[place[i] < 0 ? 0 : beside];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+      if (place[i] >= 0 && (pos[i] > above || pos[i] < from) && r + 64 * i + lane < r1) keys[r + 64 * i + lane] = kSureKey;
+  }
+  // (a wave reads only the keys that it wrote itself: no barrier)
+  // body(row of lane 0, key) for 64 rows at a time, in order.  The rows from n on have the lowest key, and being the last
+  // ones they lose every tie.
+  auto over_rows = [&](auto body) __attribute__((always_inline)) {
+    int r = r0;
+    for (; r + 64 * 4 <= r0 + run; r += 64 * 4) {
+      unsigned key[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) key[i] = keys[r + 64 * i + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) body(r + 64 * i, key[i]);
+    }
+    for (; r < r0 + run; r += 64) body(r, keys[r + lane]);
   };
   // The key of rank keep, a byte at a time from the top: among the rows that agree with it so far, count by the next
   // byte and walk down to the one in which the rank falls.
   unsigned edge = 0;
   int rank = a.keep;  // the edge's rank among the rows that agree with it
   for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) sm_hist[tid] = 0;
+#pragma unroll
+    for (int i = 0; i < 256 * kCopies / kSelectThreads; ++i) sm_hist[i * kSelectThreads + tid] = 0;
     __syncthreads();
-    for (int r = tid; r < n; r += kSelectThreads) {
-      const unsigned key = key_of(r);
-      if (shift == 24 || (key >> (shift + 8)) == (edge >> (shift + 8))) atomicAdd(&sm_hist[(key >> shift) & 255], 1);
+    const unsigned agree = shift == 24 ? 0u : ~0u << (shift + 8);
+    over_rows([&](int, unsigned key) __attribute__((always_inline)) {
+      if (((key ^ edge) & agree) == 0) atomicAdd(&sm_hist[((key >> shift) & 255) * kCopies + lane % kCopies], 1);
+    });
+    __syncthreads();
+    if (tid < 256) {
+      int sum = 0;
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) sum += sm_hist[tid * kCopies + (i + tid) % kCopies];
+      sm_hist[tid * kCopies] = sum;
     }
     __syncthreads();
     if (wave == 0) {  // lane i has the counts of bytes 255 - 4 i .. 252 - 4 i
       int own[4], sum = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        own[j] = sm_hist[255 - 4 * lane - j];
+        own[j] = sm_hist[(255 - 4 * lane - j) * kCopies];
         sum += own[j];
       }
       int incl = sum;
@@ -92,64 +181,82 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
         while (j < 3 && above + own[j] < rank) above += own[j++];
         sm_pick[0] = 255 - 4 * lane - j;
         sm_pick[1] = rank - above;
+        sm_pick[2] = rank - above == own[j];
       }
     }
     __syncthreads();
     edge |= (unsigned)sm_pick[0] << shift;
     rank = sm_pick[1];
-    __syncthreads();
+    if (sm_pick[2] && edge) {  // all rows that agree so far stay: those above the key before the lowest such one
+      --edge;
+      rank = 0;
+      break;
+    }
   }
-  // `rank` rows with the edge's key stay.  Wave x lists a run of rows of its own: first how many edge keys lie before it.
-  const int run = (n + kSelectThreads - 1) / kSelectThreads * 64;
-  const int r0 = wave * run, r1 = r0 + run < n ? r0 + run : n;
-  int ties = 0;
-  for (int r = r0; r < r1; r += 64) ties += __popcll(__builtin_amdgcn_ballot_w64(r + lane < r1 && key_of(r + lane) == edge));
-  if (lane == 0) sm_part[wave] = ties;
+  // `rank` rows with the edge's key stay, the lowest ones.  Every wave counts its rows above the edge and on it, below
+  // row keep and from there on; what the waves before it counted says where its places and movers are listed.
+  int over_lo = 0, on_lo = 0, over_hi = 0, on_hi = 0;
+  over_rows([&](int r, unsigned key) __attribute__((always_inline)) {
+    const unsigned long long over = __builtin_amdgcn_ballot_w64(key > edge), on = __builtin_amdgcn_ballot_w64(key == edge);
+    const unsigned long long lo = r + 64 <= a.keep ? ~0ull : r >= a.keep ? 0ull : (1ull << (a.keep - r)) - 1;
+    over_lo += __popcll(over & lo);
+    on_lo += __popcll(on & lo);
+    over_hi += __popcll(over & ~lo);
+    on_hi += __popcll(on & ~lo);
+  });
+  if (lane == 0) *(int4 *)sm_part[wave] = int4{over_lo, on_lo, over_hi, on_hi};
   __syncthreads();
-  int ties_before = 0;
-  for (int x = 0; x < wave; ++x) ties_before += sm_part[x];
-  __syncthreads();
-  const unsigned long long below = (1ull << lane) - 1;
-  int places = 0, movers = 0;
+  // lane x < kSelectWaves: wave x's counts; seen: rows on the edge before its rows
+  const int4 part = *(const int4 *)sm_part[lane % kSelectWaves];
+  auto before_wave = [&](int v) __attribute__((always_inline)) {  // sum over the lanes below, of those kSelectWaves
+    int incl = v;
+#pragma unroll
+    for (int sh = 1; sh < kSelectWaves; sh <<= 1) {
+      const int up = __shfl_up(incl, sh, kSelectWaves);
+      if (lane % kSelectWaves >= sh) incl += up;
+    }
+    return incl - v;
+  };
+  auto of_wave = [&](int v, int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, x); };
+  const int on_before = before_wave(part.y + part.w);
+  const int first = (lane % kSelectWaves) * run, lo_rows = min(max(a.keep - first, 0), run);
+  const int own_places = lo_rows - part.x - min(max(rank - on_before, 0), part.y);
+  const int own_movers = part.z + min(max(rank - on_before - part.y, 0), part.w);
+  const int places_before = before_wave(own_places), movers_before = before_wave(own_movers);
+  int seen = of_wave(on_before, wave), places = of_wave(places_before, wave), movers = of_wave(movers_before, wave);
+  if (tid == 0) {
+    const int all = of_wave(movers_before + own_movers, kSelectWaves - 1);
+    a.moves[w] = all < a.most_moves ? all : a.most_moves;
+  }
+  auto before = [](unsigned long long m) __attribute__((always_inline)) {  // set bits of lanes below this one
+    return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u));
+  };
   int *place_list = a.lists + (long long)w * 2 * a.most_moves, *mover_list = place_list + a.most_moves;
-  for (int pass = 0; pass < 2; ++pass) {
-    int seen = ties_before;
-    for (int r = r0; r < r1; r += 64) {
-      const bool in = r + lane < r1;
-      const unsigned key = in ? key_of(r + lane) : 0u;
-      const unsigned long long tie = __builtin_amdgcn_ballot_w64(in && key == edge);
-      const bool stays = in && (key > edge || (key == edge && seen + __popcll(tie & below) < rank));
+  over_rows([&](int r, unsigned key) __attribute__((always_inline)) {
+    unsigned long long stays = __builtin_amdgcn_ballot_w64(key > edge);
+    const unsigned long long tie = __builtin_amdgcn_ballot_w64(key == edge);
+    if (tie) {
+      stays |= __builtin_amdgcn_ballot_w64(key == edge && seen + before(tie) < rank);
       seen += __popcll(tie);
-      const bool is_place = in && !stays && r + lane < a.keep, is_mover = stays && r + lane >= a.keep;
-      const unsigned long long pm = __builtin_amdgcn_ballot_w64(is_place), mm = __builtin_amdgcn_ballot_w64(is_mover);
-      if (pass == 1) {
-        const int ip = places + __popcll(pm & below), im = movers + __popcll(mm & below);
-        if (is_place && ip < a.most_moves) place_list[ip] = r + lane;
-        if (is_mover && im < a.most_moves) mover_list[im] = r + lane;
-      }
+    }
+    const unsigned long long lo = r + 64 <= a.keep ? ~0ull : r >= a.keep ? 0ull : (1ull << (a.keep - r)) - 1;
+    const unsigned long long pm = ~stays & lo, mm = stays & ~lo;
+    if (pm) {
+      const int i = places + before(pm);
+      if (((pm >> lane) & 1) && i < a.most_moves) place_list[i] = r + lane;
       places += __popcll(pm);
+    }
+    if (mm) {
+      const int i = movers + before(mm);
+      if (((mm >> lane) & 1) && i < a.most_moves) mover_list[i] = r + lane;
       movers += __popcll(mm);
     }
-    if (pass == 1) break;
-    if (lane == 0) {
-      sm_part[wave] = places;
-      sm_part2[wave] = movers;
-    }
-    __syncthreads();
-    places = movers = 0;
-    int all = 0;
-    for (int x = 0; x < kSelectWaves; ++x) {
-      if (x < wave) {
-        places += sm_part[x];
-        movers += sm_part2[x];
-      }
-      all += sm_part2[x];
-    }
-    if (tid == 0) a.moves[w] = all < a.most_moves ? all : a.most_moves;
-  }
+  });
 }
 
-// D * 2 (D for e4m3) bytes of keys and values per row, 16 a lane.
+// Rows of keys and values (2 D bytes each, D as e4m3), 16 bytes a lane; kMovesAtOnce rows of a lane are under way
+// together, since each is a chain of three accesses: lists, table, row.
+constexpr int kMovesAtOnce = 4;
 __global__ __launch_bounds__(256) void paged_move_kernel(const PagedEvictArgs a) {
   const int w = blockIdx.x, b = w / a.Hkv, h = w - b * a.Hkv;
   const int count = a.moves[w];
@@ -158,27 +265,76 @@ __global__ __launch_bounds__(256) void paged_move_kernel(const PagedEvictArgs a)
   const int *table = table_of(a.c, a.Hkv, b, h);
   const int *place_list = a.lists + (long long)w * 2 * a.most_moves, *mover_list = place_list + a.most_moves;
   unsigned char *pool = is_v ? a.c.v : a.c.k;
-  for (int i = blockIdx.y * per + mine; i < count; i += gridDim.y * per) {
-    int to_row, of_row;
-    const int to = page_of(a.c, table, place_list[i], to_row), of = page_of(a.c, table, mover_list[i], of_row);
-    if (to < 0 || of < 0) continue;
-    *(uint4 *)(pool + row_offset(a.c, to, h, to_row) + 16 * piece) = *(const uint4 *)(pool + row_offset(a.c, of, h, of_row) + 16 * piece);
-    if (piece == 0) {
-      const long long p1 = row_place(a.c, to, h, to_row), p0 = row_place(a.c, of, h, of_row);
-      if (a.c.e4m3) (is_v ? a.c.v_scale : a.c.k_scale)[p1] = (is_v ? a.c.v_scale : a.c.k_scale)[p0];
-      if (is_v) a.c.mass[p1] = a.c.mass[p0];
-      else a.c.pos[p1] = a.c.pos[p0];
+  unsigned char *scale = is_v ? a.c.v_scale : a.c.k_scale;
+  unsigned *per_row = is_v ? (unsigned *)a.c.mass : (unsigned *)a.c.pos;  // of a row, the lanes of its values take the one along, those of its keys the other
+  for (int i0 = blockIdx.y * per * kMovesAtOnce + mine; i0 < count; i0 += gridDim.y * per * kMovesAtOnce) {
+    long long to[kMovesAtOnce], of[kMovesAtOnce], to_place[kMovesAtOnce], of_place[kMovesAtOnce];
+    u32x4 x[kMovesAtOnce];
+    unsigned beside[kMovesAtOnce];
+    unsigned char byte[kMovesAtOnce];
+    int to_row[kMovesAtOnce], of_row[kMovesAtOnce];
+#pragma unroll
+    for (int m = 0; m < kMovesAtOnce; ++m) {
+      const int i = i0 + m * per < count ? i0 + m * per : i0;
+      to_row[m] = place_list[i];
+      of_row[m] = mover_list[i];
+    }
+#pragma unroll
+    for (int m = 0; m < kMovesAtOnce; ++m) {
+      int in_page;
+      int page = page_of(a.c, table, to_row[m], in_page);
+      to[m] = page < 0 ? -1 : row_offset(a.c, page, h, in_page);
+      to_place[m] = row_place(a.c, page, h, in_page);
+      page = page_of(a.c, table, of_row[m], in_page);
+      if (page < 0) to[m] = -1;
+      of[m] = page < 0 ? 0 : row_offset(a.c, page, h, in_page);
+      of_place[m] = row_place(a.c, page, h, in_page);
+    }
+#pragma unroll
+    for (int m = 0; m < kMovesAtOnce; ++m) {
+      x[m] = __builtin_nontemporal_load((const u32x4 *)(pool + of[m] + 16 * piece));
+      if (piece == 0) {
+        beside[m] = per_row[to[m] < 0 ? 0 : of_place[m]];
+        if (a.c.e4m3) byte[m] = scale[to[m] < 0 ? 0 : of_place[m]];
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < kMovesAtOnce; ++m) {
+      if (i0 + m * per < count && to[m] >= 0) {
+        __builtin_nontemporal_store(x[m], (u32x4 *)(pool + to[m] + 16 * piece));
+        if (piece == 0) {
+          per_row[to_place[m]] = beside[m];
+          if (a.c.e4m3) scale[to_place[m]] = byte[m];
+        }
+      }
     }
   }
 }
 
+bool evict_keys_held(long long max_rows) { return max_rows <= kHeldRows; }
+
 hipError_t launch_paged_evict(const PagedEvictArgs &a, hipStream_t st) {
   const int windows = a.B * a.Hkv;
-  hipLaunchKernelGGL(paged_select_kernel, dim3(windows), dim3(kSelectThreads), 0, st, a);
+  const bool in_page = a.c.page_rows.d % 64 == 0;
+  if (a.keys) {
+    const auto kern = in_page ? paged_select_kernel<false, true> : paged_select_kernel<false, false>;
+    hipLaunchKernelGGL(kern, dim3(windows), dim3(kSelectThreads), 0, st, a);
+  } else {
+    const auto kern = in_page ? paged_select_kernel<true, true> : paged_select_kernel<true, false>;
+    static std::atomic<bool> allowed[2];
+    if (!allowed[in_page].load(std::memory_order_acquire)) {
+      const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kHeldRows * 4);
+      if (e != hipSuccess) return e;
+      allowed[in_page].store(true, std::memory_order_release);
+    }
+    const int lds = a.most_moves ? (a.max_rows + kSelectThreads - 1) / kSelectThreads * kSelectThreads * 4 : 0;  // no window can hold more than it may: nothing is selected
+    hipLaunchKernelGGL(kern, dim3(windows), dim3(kSelectThreads), lds, st, a);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.most_moves == 0) return e;
-  int wgs = 4096 / windows;
-  const int most = (a.most_moves + 7) / 8;
+  int wgs = 16384 / windows;
+  const int at_once = kMovesAtOnce * 256 / (a.D * (a.c.e4m3 ? 2 : 4) / 16);  // rows of a workgroup
+  const int most = (a.most_moves + at_once - 1) / at_once;
   wgs = wgs < 1 ? 1 : wgs > most ? most : wgs;
   hipLaunchKernelGGL(paged_move_kernel, dim3(windows, wgs), dim3(256), 0, st, a);
   return hipGetLastError();
