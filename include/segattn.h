@@ -474,7 +474,8 @@ segattn_status seg_kv_paged_append(const segattn_config *cfg, const segattn_page
  * zeros and -infinity.  max_rows (host, <= max_pages * page_rows): the most rows of a head; it sizes the launch
  * and the workspace, and of a head that holds more only the first max_rows are seen.  accumulate = 1: pages->mass
  * of every row of a PAST head grows by the weight that the row has for this token, summed over the query heads
- * of its group (at least one PAST head; EINVAL without mass).  At most 128 query heads per KV head.
+ * of its group (at least one PAST head, max_rows times the heads of a group below 2^29 -
+ * 2^12; EINVAL without mass).  At most 128 query heads per KV head.
  * workspace: device, >= ..._workspace_bytes() (0: invalid arguments), 256-byte aligned, overwritten: calls that
  * may overlap need one each. */
 size_t seg_attn_decode_paged_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,

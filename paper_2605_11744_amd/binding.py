@@ -129,11 +129,12 @@ EXPORTS = ("segattn_cache_bytes", "segattn_create", "segattn_destroy", "segattn_
 
 
 def _ptr(x) -> Optional[int]:
-    if x is None:
-        return None
-    if hasattr(x, "data_ptr"):
+    if x is None or type(x) is int:
+        return x
+    try:
         return x.data_ptr()
-    return int(x)
+    except AttributeError:
+        return int(x)
 
 
 def _check(st: int, where: str) -> None:

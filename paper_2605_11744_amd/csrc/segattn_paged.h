@@ -108,7 +108,7 @@ struct PagedDecodeArgs {
   float *lse;
   int2 *pieces;         // workspace: first and last slot of every window
   float *slots;         // workspace: partials [slot][g][ws_slot_floats(D)]
-  float *scores;        // workspace: [B, n_past][g][score_rows], or nullptr
+  float *scores;        // workspace: [B, n_past][score_rows / tile][g][tile], or nullptr
   long long score_rows;
   int B, Hq, Hkv, g, D, n_windows, n_past;
   int max_rows, tail;

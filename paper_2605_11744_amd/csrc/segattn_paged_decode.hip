@@ -138,37 +138,41 @@ __device__ inline float over_quads(float x, bool sum) {  // over the four lanes 
 }
 
 // kInPage: page_rows is a multiple of the tile, so a tile lies in one page; otherwise every row asks the table.
-template <int D, bool kE4m3, bool kInPage>
+// kMass: the scores are left for the weights.
+template <int D, bool kE4m3, bool kInPage, bool kMass>
 __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedDecodeArgs a) {
   constexpr int NK = D / 32, NB = D / 16;
   constexpr int kRow = 2 * D, kTileBytes = kPagedTile * kRow;  // of a tile in LDS, bf16
   constexpr int kPieces = (kE4m3 ? D : 2 * D) / 16;            // 16-byte pieces of a row in memory
   constexpr int RPL = 64 / kPieces, NL = kPagedTile / RPL;     // rows per wave load, loads per tile and tensor
-  // XOR on the number of a row's 16-byte chunk: 16 rows read at one chunk (K), or 8 rows at two (V), meet every bank once
-  auto swz_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
-  auto swz_v = [](int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
+  // Where a row's 16-byte chunk lies: XORed so that 16 rows read at one chunk (K), or 8 rows at two (V), meet every bank once,
+  // and so do the eight lanes that write every other chunk of an 8-bit row (its upper half is flipped against the lower one).
+  auto chunk_k = [](int row, int chunk) { return D == 128 ? chunk ^ (chunk >> 3) ^ (row & 15) : chunk ^ ((row >> 1) & 7); };
+  auto chunk_v = [](int row, int chunk) { return D == 128 ? chunk ^ (chunk >> 3) ^ (2 * (row & 7)) : chunk ^ (2 * ((row >> 1) & 3)); };
 
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int quad = lane >> 4, col = lane & 15;
   const float c = a.scale_log2e;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[kPagedWaves][2 * kTileBytes];
   constexpr int MS = D + 4;  // floats per head of the merge area
   static_assert(kPagedWaves * 2 * kTileBytes >= (int)sizeof(float) * kPagedWaves * kPagedHeads * MS, "merge area fits the tiles");
 
-  const PagedSlice slice = paged_slice(a, gridDim.x);
+  PagedSlice slice = paged_slice(a, gridDim.x);
+  slice.w = __builtin_amdgcn_readfirstlane(slice.w);  // the same in all lanes: what follows from them is scalar work
+  slice.tile = __builtin_amdgcn_readfirstlane(slice.tile);
+  slice.count = __builtin_amdgcn_readfirstlane(slice.count);
   if (slice.w < 0) return;
   const int pass = blockIdx.y, live = min(kPagedHeads, a.g - pass * kPagedHeads);
   unsigned char *tile = tiles[wave];
-  int koff[2][NK], voff[2][NB];
+  const unsigned char *scales = lane < 32 ? a.c.k_scale : a.c.v_scale;
+  // where this lane reads its operands; the tile's second 16 rows lie 16 kRow further on (both XORs repeat after 16 rows)
+  int koff[NK], voff[NB];
+  const int vrow = 4 * quad + (col >> 2);
 #pragma unroll
-  for (int h2 = 0; h2 < 2; ++h2) {
-    const int krow = 16 * h2 + col, vrow = 16 * h2 + 4 * quad + (col >> 2);
+  for (int kc = 0; kc < NK; ++kc) koff[kc] = col * kRow + (chunk_k(col, 4 * kc + quad) << 4);
 #pragma unroll
-    for (int kc = 0; kc < NK; ++kc) koff[h2][kc] = krow * kRow + (((4 * kc + quad) ^ swz_k(krow)) << 4);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-      voff[h2][nb] = kTileBytes + vrow * kRow + (((2 * nb + ((col & 3) >> 1)) ^ swz_v(vrow)) << 4) + 8 * (col & 1);
-  }
+  for (int nb = 0; nb < NB; ++nb)
+    voff[nb] = kTileBytes + vrow * kRow + (chunk_v(vrow, 2 * nb + ((col & 3) >> 1)) << 4) + 8 * (col & 1);
 
   int left = slice.count;
   for (int w = slice.w, tile0 = slice.tile; left > 0 && w < a.n_windows; ++w, tile0 = 0) {
@@ -200,14 +204,10 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
     for (int nb = 0; nb < NB; ++nb) O[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, l_run = 0.f;
 
-    float *scores = nullptr;
-    if (a.scores && in_set(a.heads.past, h) && col < live)
-      scores = a.scores + ((long long)(b * a.n_past + set_before(a.heads.past, h)) * a.g + pass * kPagedHeads + col) * a.score_rows;
-
-    u32x4 nk[NL], nv[NL];     // the wave's next tile, in flight
-    int n_scale = 0;          // scale byte of row lane % 32: keys in the lower half of the wave, values in the upper
-    unsigned n_valid = 0;     // rows of it that count
-    int entry = 0, entry_row = 0;  // the table's entry for the tile after that (kInPage), or for this lane's row of it
+    u32x4 nk[NL], nv[NL];          // the wave's next tile, in flight
+    int n_scale = 0;               // scale byte of row lane % 32: keys in the lower half of the wave, values in the upper
+    unsigned n_valid = 0;          // rows of it that count
+    int entry = 0, entry_row = 0;  // the table's entry for the tile that is fetched next (kInPage), or for this lane's row of it
     auto ask = [&](int t) __attribute__((always_inline)) {
       if constexpr (kInPage) {
         entry = table[fast_div(t * kPagedTile, a.c.page_rows)];
@@ -228,19 +228,19 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
       const int page = named ? entry : 0;  // rows without a page: some row that exists, with weight 0
       if constexpr (kInPage) {
         const int pg = __builtin_amdgcn_readfirstlane(page);
-        if (!__builtin_amdgcn_readfirstlane(named)) valid = 0;
+        if (!__builtin_amdgcn_readfirstlane((int)named)) valid = 0;
         const int in_page = r0 - fast_div(r0, a.c.page_rows) * (int)a.c.page_rows.d;
         const long long at = pg * a.c.page_bytes + hh * a.c.head_bytes + in_page * a.c.row_bytes;
         const unsigned mine = (unsigned)(lane / kPieces) * (unsigned)a.c.row_bytes + (lane % kPieces) * 16;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-          const long long step = at + i * (RPL * a.c.row_bytes);
-          nk[i] = __builtin_nontemporal_load((const u32x4 *)(a.c.k + step + mine));
-          nv[i] = __builtin_nontemporal_load((const u32x4 *)(a.c.v + step + mine));
+          const unsigned char *k = a.c.k + at + i * (RPL * a.c.row_bytes), *v = a.c.v + at + i * (RPL * a.c.row_bytes);
+          nk[i] = __builtin_nontemporal_load((const u32x4 *)(k + mine));
+          nv[i] = __builtin_nontemporal_load((const u32x4 *)(v + mine));
         }
         if constexpr (kE4m3) {
           const long long place = ((long long)pg * a.c.heads + hh) * a.c.page_rows.d + in_page + (lane & 31);
-          n_scale = (lane < 32 ? a.c.k_scale : a.c.v_scale)[place];
+          n_scale = scales[place];
         }
       } else {
         valid &= (unsigned)__builtin_amdgcn_ballot_w64(named);
@@ -253,22 +253,20 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
         }
         if constexpr (kE4m3) {
           const long long place = ((long long)page * a.c.heads + hh) * a.c.page_rows.d + entry_row;
-          n_scale = (lane < 32 ? a.c.k_scale : a.c.v_scale)[place];
+          n_scale = scales[place];
         }
       }
       n_valid = valid;
     };
-    // A tile into LDS; rows that do not count as zeros (a weight of zero times NaN would be NaN).
-    auto stage = [&](unsigned valid) __attribute__((always_inline)) {
-      const bool whole = valid == ~0u;
+    // A tile into LDS, values of rows that do not count as zeros (a weight of zero times NaN would be NaN).
+    auto stage = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int r = RPL * i + lane / kPieces, piece = lane % kPieces;
-        u32x4 xk = nk[i], xv = nv[i];
-        if (!whole && !((valid >> r) & 1)) xk = xv = u32x4{0u, 0u, 0u, 0u};
+        const u32x4 xk = nk[i], xv = nv[i];
         if constexpr (!kE4m3) {
-          *(u32x4 *)(tile + r * kRow + ((piece ^ swz_k(r)) << 4)) = xk;
-          *(u32x4 *)(tile + kTileBytes + r * kRow + ((piece ^ swz_v(r)) << 4)) = xv;
+          *(u32x4 *)(tile + r * kRow + (chunk_k(r, piece) << 4)) = xk;
+          *(u32x4 *)(tile + kTileBytes + r * kRow + (chunk_v(r, piece) << 4)) = xv;
         } else {
           // a scale is a power of two and e4m3 has four significant bits: the bf16 is exact
           const float sk = __uint_as_float((unsigned)__shfl(n_scale, r) << 23), sv = __uint_as_float((unsigned)__shfl(n_scale, r + 32) << 23);
@@ -283,33 +281,44 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
               yv[2 * e + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(xv[2 * half + e], sv, true);
             }
             const int chunk = 2 * piece + half;
-            *(u32x4 *)(tile + r * kRow + ((chunk ^ swz_k(r)) << 4)) = __builtin_bit_cast(u32x4, yk);
-            *(u32x4 *)(tile + kTileBytes + r * kRow + ((chunk ^ swz_v(r)) << 4)) = __builtin_bit_cast(u32x4, yv);
+            *(u32x4 *)(tile + r * kRow + (chunk_k(r, chunk) << 4)) = __builtin_bit_cast(u32x4, yk);
+            *(u32x4 *)(tile + kTileBytes + r * kRow + (chunk_v(r, chunk) << 4)) = __builtin_bit_cast(u32x4, yv);
           }
         }
       }
+      if (n_valid != ~0u && !((n_valid >> (lane & 31)) & 1)) {
+#pragma unroll
+        for (int i = 0; i < kRow / 32; ++i)
+          *(u32x4 *)(tile + kTileBytes + (lane & 31) * kRow + (kRow / 32 * (lane >> 5) + i) * 16) = u32x4{0u, 0u, 0u, 0u};
+      }
     };
 
-    int t = t_begin + wave;
-    if (t < t_end) {
-      ask(t);
-      fetch(t);
-      if (t + kPagedWaves < t_end) ask(t + kPagedWaves);
+    // Scores of a PAST head's rows for the weights, [tile][head][row of the tile]: 16 bytes a lane, written through a buffer that
+    // ends with the window's scores and is empty for other heads, so that every step issues the same stores -- with a
+    // branch around them the wait for the next tile would be one for the stores too.
+    __amdgpu_buffer_rsrc_t score_rsrc;
+    int score_at = 0;
+    const int score_tile = a.g * kPagedTile * 4;  // bytes
+    if constexpr (kMass) {
+      const bool past = in_set(a.heads.past, h);
+      float *scores = a.scores + (long long)(b * a.n_past + (past ? set_before(a.heads.past, h) : 0)) * a.g * a.score_rows;
+      score_rsrc = __builtin_amdgcn_make_buffer_rsrc(scores, 0, past ? a.g * (int)a.score_rows * 4 : 0, 0x00020000);
+      score_at = col < live ? ((pass * kPagedHeads + col) * kPagedTile + 4 * quad) * 4 : (int)0x80000000;  // out of range for columns without a head
     }
-    for (; t < t_end; t += kPagedWaves) {
-      const unsigned valid = n_valid;
-      stage(valid);
-      if (t + kPagedWaves < t_end) {
-        fetch(t + kPagedWaves);
-        if (t + 2 * kPagedWaves < t_end) ask(t + 2 * kPagedWaves);
-      }
+    auto store_scores = [&](int t, const f32x4 (&x)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x[h2]), score_rsrc, score_at + t * score_tile + 64 * h2, 0, 0);
+    };
+
+    auto products = [&](int t, unsigned valid) __attribute__((always_inline)) {
       f32x4 S[2];
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2) {
         S[h2] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kc = 0; kc < NK; ++kc)
-          S[h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)(tile + koff[h2][kc]), Q[kc], S[h2], 0, 0, 0);
+          S[h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)(tile + koff[kc] + 16 * h2 * kRow), Q[kc], S[h2], 0, 0, 0);
       }
       // register r of S[h2] is key 16 h2 + 4 quad + r
       if (valid != ~0u) {
@@ -319,10 +328,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
           for (int r = 0; r < 4; ++r)
             if (!((valid >> (16 * h2 + 4 * quad + r)) & 1)) S[h2][r] = -INFINITY;
       }
-      if (scores) {
-#pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) *(f32x4 *)(scores + t * kPagedTile + 16 * h2 + 4 * quad) = S[h2];
-      }
+      if constexpr (kMass) store_scores(t, S);
       float mx = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
       mx = over_quads(mx, false);
       const float m_new = fmaxf(m_run, mx);
@@ -341,15 +347,44 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
           P_rest[4 * h2 + r] = (__bf16)(e - (float)P[4 * h2 + r]);
         }
       l_run = l_run * alpha + sum;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {  // a new maximum somewhere: rare behind the first tiles
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) O[nb] *= alpha;
+      }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        O[nb] *= alpha;
-        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[0][nb]));
-        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[1][nb]));
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[nb]));
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[nb] + 16 * kRow));
         const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
         O[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, P, O[nb], 0, 0, 0);
         O[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, P_rest, O[nb], 0, 0, 0);
       }
+    };
+
+    int t = t_begin + wave;
+    if (t < t_end) {
+      ask(t);
+      fetch(t);
+      ask(min(t + kPagedWaves, t_end - 1));
+      if constexpr (kMass) {  // two stores that go nowhere: as many accesses behind the loads as in the loop
+        const f32x4 none[2] = {};
+        const int at = score_at;
+        score_at = (int)0x80000000;
+        store_scores(t, none);
+        score_at = at;
+      }
+      // The last tile by itself: with the next one's loads under a condition in the loop the scales of 8-bit rows are
+      // copied to where they are used as soon as they are there, and the loop waits for what it should only have asked for
+      // (24 sequences of 1K to 32K rows, weights added up: 175 us).
+      for (; t + kPagedWaves < t_end; t += kPagedWaves) {
+        const unsigned valid = n_valid;
+        stage();
+        fetch(t + kPagedWaves);
+        ask(min(t + 2 * kPagedWaves, t_end - 1));
+        products(t, valid);
+      }
+      stage();
+      products(t, n_valid);
     }
     l_run = over_quads(l_run, true);
 
@@ -416,6 +451,7 @@ __device__ inline void joined_sum(const float *ml, long long stride, int count, 
   }
 }
 
+constexpr int kJoinBatch = 8;    // partials of a wave under way together
 constexpr int kMassRows = 1024;  // rows a workgroup adds the weights of
 
 // Workgroups 0 .. B Hq - 1: merge of one query head's partials.  The others: weights of kMassRows rows of one PAST
@@ -436,15 +472,33 @@ __global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecod
     float top = -INFINITY, l = 0.f, o[DPL];
 #pragma unroll
     for (int e = 0; e < DPL; ++e) o[e] = 0.f;
-    for (int s = wave; s < count; s += 4) {
-      const float *src = ws + (long long)s * a.g * SF;
-      const float2 ml = *(const float2 *)(src + D);
-      const float m_new = fmaxf(top, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
-      const float keep = __builtin_amdgcn_exp2f((top - ref) * c), wgt = __builtin_amdgcn_exp2f((ml.x - ref) * c);
-      top = m_new;
-      l = l * keep + ml.y * wgt;
+    for (int s0 = wave; s0 < count; s0 += 4 * kJoinBatch) {  // (one memory round trip for up to 4 kJoinBatch partials)
+      float2 ml[kJoinBatch];
+      float x[kJoinBatch][DPL];
 #pragma unroll
-      for (int e = 0; e < DPL; ++e) o[e] = o[e] * keep + src[lane * DPL + e] * wgt;
+      for (int i = 0; i < kJoinBatch; ++i) {
+        const float *src = ws + (long long)(s0 + 4 * i < count ? s0 + 4 * i : count - 1) * a.g * SF;
+        ml[i] = *(const float2 *)(src + D);
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) x[i][e] = src[lane * DPL + e];
+      }
+      float m_new = top;
+#pragma unroll
+      for (int i = 0; i < kJoinBatch; ++i) m_new = fmaxf(m_new, ml[i].x);  // (the last one again changes nothing)
+      const float ref = m_new == -INFINITY ? 0.f : m_new, keep = __builtin_amdgcn_exp2f((top - ref) * c);
+      top = m_new;
+      l *= keep;
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) o[e] *= keep;
+#pragma unroll
+      for (int i = 0; i < kJoinBatch; ++i) {
+        if (s0 + 4 * i < count) {
+          const float wgt = __builtin_amdgcn_exp2f((ml[i].x - ref) * c);
+          l += ml[i].y * wgt;
+#pragma unroll
+          for (int e = 0; e < DPL; ++e) o[e] += x[i][e] * wgt;
+        }
+      }
     }
     if (lane == 0) {
       sm_m[wave] = top;
@@ -478,7 +532,25 @@ __global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecod
     if (in_set(a.heads.past, h) && k-- == 0) break;
   const int w = b * a.Hkv + h, n = rows_held(a.rows, w, a.max_rows);
   if (chunk * kMassRows >= n) return;
+  // A thread has four consecutive rows.  What it reads is asked for before the sums are joined, which takes a chain of loads too.
   __shared__ float sm_top[kPagedMostGroup], sm_share[kPagedMostGroup];
+  const int r0 = chunk * kMassRows + 4 * tid;
+  const int *table = table_of(a.c, a.Hkv, b, h);
+  const int rs = r0 < n ? r0 : 0;  // (the rows up to a whole tile are there)
+  const float *scores = a.scores + ((long long)win * a.score_rows + rs / kPagedTile * kPagedTile) * a.g + rs % kPagedTile;
+  long long place[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    int in_page;
+    const int page = r0 + x < n ? page_of(a.c, table, r0 + x, in_page) : -1;
+    place[x] = page < 0 ? -1 : row_place(a.c, page, h, in_page);
+  }
+  float4 first[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) first[j] = *(const float4 *)(scores + (j < a.g ? j : 0) * kPagedTile);
+  float mass[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) mass[x] = a.c.mass[place[x] < 0 ? 0 : place[x]];
   const int2 piece = a.pieces[w];
   for (int j = wave; j < a.g; j += 4) {
     float top, l;
@@ -489,22 +561,26 @@ __global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecod
     }
   }
   __syncthreads();
-  const int *table = table_of(a.c, a.Hkv, b, h);
-  const float *scores = a.scores + (long long)win * a.g * a.score_rows;
-  for (int r = chunk * kMassRows + tid; r < n && r < (chunk + 1) * kMassRows; r += 256) {
-    int in_page;
-    const int page = page_of(a.c, table, r, in_page);
-    if (page < 0) continue;
-    float sum = 0.f;
-    for (int j = 0; j < a.g; ++j) sum += __builtin_amdgcn_exp2f((scores[j * a.score_rows + r] - sm_top[j]) * c) * sm_share[j];
-    a.c.mass[row_place(a.c, page, h, in_page)] += sum;
-  }
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](float4 s, int j) __attribute__((always_inline)) {
+    sum[0] += __builtin_amdgcn_exp2f((s.x - sm_top[j]) * c) * sm_share[j];
+    sum[1] += __builtin_amdgcn_exp2f((s.y - sm_top[j]) * c) * sm_share[j];
+    sum[2] += __builtin_amdgcn_exp2f((s.z - sm_top[j]) * c) * sm_share[j];
+    sum[3] += __builtin_amdgcn_exp2f((s.w - sm_top[j]) * c) * sm_share[j];
+  };
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (j < a.g) add(first[j], j);
+  for (int j = 4; j < a.g; ++j) add(*(const float4 *)(scores + j * kPagedTile), j);
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+    if (place[x] >= 0) a.c.mass[place[x]] = mass[x] + sum[x];
 }
 
-template <int D, bool kE4m3, bool kInPage>
+template <int D, bool kE4m3, bool kInPage, bool kMass>
 static hipError_t launch_split(PagedDecodeArgs a, hipStream_t st) {
   static ResidentCount count;
-  const auto kern = paged_decode_split_kernel<D, kE4m3, kInPage>;
+  const auto kern = paged_decode_split_kernel<D, kE4m3, kInPage, kMass>;
   const int resident = count.get((const void *)kern, 256, 0);
   if (resident == 0) return hipErrorUnknown;
   long long grid = resident < kPagedMostWgs ? resident : kPagedMostWgs;
@@ -515,6 +591,10 @@ static hipError_t launch_split(PagedDecodeArgs a, hipStream_t st) {
   else if (a.n_windows <= kPagedLaneWindows && grid < 2 * a.n_windows) grid = 2 * a.n_windows;  // paged_slice needs spare ones
   hipLaunchKernelGGL(kern, dim3((unsigned)grid, (a.g + kPagedHeads - 1) / kPagedHeads), dim3(256), 0, st, a);
   return hipGetLastError();
+}
+template <int D, bool kE4m3, bool kInPage>
+static hipError_t launch_split(const PagedDecodeArgs &a, hipStream_t st) {
+  return a.scores ? launch_split<D, kE4m3, kInPage, true>(a, st) : launch_split<D, kE4m3, kInPage, false>(a, st);
 }
 template <int D>
 static hipError_t launch_paged(const PagedDecodeArgs &a, hipStream_t st) {

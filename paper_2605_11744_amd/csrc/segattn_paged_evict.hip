@@ -18,8 +18,8 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr unsigned kSureKey = 0xffffffffu;
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kHeldRows = 32 * kSelectThreads;  // rows whose keys fit the select kernel's LDS
-constexpr int kCopies = 16;       // of the histogram: neighbouring lanes count in different ones
-constexpr int kAtOnce = 8;        // rows of a lane that are under way together
+constexpr int kCopies = 4;        // of the histogram: neighbouring lanes count in different ones
+constexpr int kAtOnce = 4;        // rows of a lane that are under way together
 
 // The select kernel walks over a window's keys seven times, so they are formed once (a key costs a look into the
 // table and two loads) and kept: in LDS (kHeld), or for longer windows in the workspace.  Wave x has a run of consecutive
