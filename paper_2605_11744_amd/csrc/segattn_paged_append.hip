@@ -6,11 +6,13 @@
 // element rounded once, and e4m3's range loses less than a factor of two of the 2^15 that it spans.  With a
 // row: its position, and a weight of zero.  Every input is read and every output written once; bound by
 // memory, a generation step by the chain row count -> page -> store.
+#include <utility>
+
 #include "segattn_rotate.h"
 
 namespace segattn {
 
-constexpr int kAppendRows = 16;
+constexpr int kAppendRows = 4;  // (prompts into an 8-bit cache 100 us with 16, 90 with 4, 91 with 2, 99 with 1)
 
 // Exponent e of the scale of a row whose largest finite magnitude is `most`, as the byte e + 127: the binary
 // exponent of most minus that of 448 = 1.75 * 2^8, one more where the significand is above 1.75.  Rows
@@ -42,7 +44,7 @@ __device__ inline uint2 e4m3_of(const float *x, float inverse) {
 // (token, head)'s row, and forms the sines, in LDS; then its threads walk over the units of the queries, the
 // keys and the values.  The D / 16 threads of a row are neighbours in one wave, which finds an e4m3 row's
 // largest magnitude by exchanges between lanes.
-template <int D, bool kE4m3>
+template <int D, bool kE4m3, bool kInterleaved>
 __global__ __launch_bounds__(256) void paged_append_kernel(const PagedAppendArgs a, const int tokens_per_wg, const int token_wgs) {
   constexpr int kUnits = D / 16;
   __shared__ __attribute__((aligned(16))) float sm_sn[kAppendRows][64], sm_cs[kAppendRows][64];
@@ -101,22 +103,17 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedAppendArgs
       a.rows_out[w] = held < a.c.cap ? held + 1 : a.c.cap;
     }
   }
-  auto turn = [&](float (&x)[16], int r, int unit) __attribute__((always_inline)) {
-    if (8 * unit < pairs) turn_unit(x, &sm_sn[r][8 * unit], &sm_cs[r][8 * unit], a.rot.interleaved);
-  };
   if (a.q_out) {
     const int per_token = a.Hq * kUnits;
     for (int j = tid; j < n * per_token; j += 256) {
       const int r = j / per_token, u = j - r * per_token, unit = u % kUnits;
       int lo, hi;
-      unit_channels(unit, pairs, a.rot.interleaved, lo, hi);
+      unit_channels<8>(unit, pairs, D, lo, hi);
       const long long at = ((long long)(t0 + r) * a.Hq + u / kUnits) * D;
-      float x[16];
-      load8(a.q + at + lo, x);
-      load8(a.q + at + hi, x + 8);
-      turn(x, r, unit);
-      store8(a.q_out + at + lo, x);
-      store8(a.q_out + at + hi, x + 8);
+      u32x4 x = load_piece(a.q + at + lo), y = load_piece(a.q + at + hi);
+      if (8 * unit < pairs) turn_pieces<8, kInterleaved>(x, y, unit, pairs, sm_sn[r], sm_cs[r]);
+      store_piece(a.q_out + at + lo, x);
+      store_piece(a.q_out + at + hi, y);
     }
   }
   const int per_token = a.Hkv * kUnits, per_tensor = n * per_token;
@@ -125,15 +122,24 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedAppendArgs
     const int jj = is_v ? j - per_tensor : j;
     const int r = jj / per_token, u = jj - r * per_token, head = u / kUnits, unit = u % kUnits;
     int lo = 16 * unit, hi = lo + 8;
-    if (!is_v) unit_channels(unit, pairs, a.rot.interleaved, lo, hi);
+    if (!is_v) unit_channels<8>(unit, pairs, D, lo, hi);
     const unsigned short *src = (is_v ? a.v : a.k) + ((long long)(t0 + r) * a.Hkv + head) * D;
-    float x[16];
-    load8(src + lo, x);
-    load8(src + hi, x + 8);
-    if (!is_v) turn(x, r, unit);
+    const u32x4 x_lo = load_piece(src + lo), x_hi = load_piece(src + hi);
     const int2 at = sm_row[r * a.Hkv + head];
     int byte = 0;
+    float x[16];
     if constexpr (kE4m3) {
+      {
+        float p[8], q[8];
+        numbers_of(x_lo, p);
+        numbers_of(x_hi, q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] = p[e];
+          x[8 + e] = q[e];
+        }
+      }
+      if (!is_v && 8 * unit < pairs) turn_unit<8, kInterleaved>(x, unit, pairs, sm_sn[r], sm_cs[r]);
       float most = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) most = fmaxf(most, finite_magnitude(x[e]));
@@ -150,8 +156,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedAppendArgs
       *(uint2 *)(dst + hi) = e4m3_of(x + 8, inverse);
       if (unit == 0) (is_v ? a.c.v_scale : a.c.k_scale)[place] = (unsigned char)byte;
     } else {
-      store8((unsigned short *)dst + lo, x);
-      store8((unsigned short *)dst + hi, x + 8);
+      u32x4 p = x_lo, q = x_hi;
+      if (!is_v && 8 * unit < pairs) turn_pieces<8, kInterleaved>(p, q, unit, pairs, sm_sn[r], sm_cs[r]);
+      store_piece((unsigned short *)dst + lo, p);
+      store_piece((unsigned short *)dst + hi, q);
     }
     if (unit == 0 && !is_v) {
       if (a.c.pos) a.c.pos[place] = (int)((a.pos0 ? a.pos0[sm_seq[r]] : 0) + sm_index[r]);
@@ -179,13 +187,12 @@ hipError_t launch_paged_append(const PagedAppendArgs &args, hipStream_t st) {
   const bool in_place = a.rows == a.rows_out;
   a.count_rows = !in_place ? 2 : (a.cu == nullptr && per == 1) ? 1 : 0;
   const int grid = wgs + (a.count_rows == 2 ? 1 : 0);
-  if (a.D == 128) {
-    if (a.c.e4m3) hipLaunchKernelGGL((paged_append_kernel<128, true>), dim3(grid), dim3(256), 0, st, a, per, wgs);
-    else hipLaunchKernelGGL((paged_append_kernel<128, false>), dim3(grid), dim3(256), 0, st, a, per, wgs);
-  } else {
-    if (a.c.e4m3) hipLaunchKernelGGL((paged_append_kernel<64, true>), dim3(grid), dim3(256), 0, st, a, per, wgs);
-    else hipLaunchKernelGGL((paged_append_kernel<64, false>), dim3(grid), dim3(256), 0, st, a, per, wgs);
-  }
+  const auto of = [&](auto turned) { return a.rot.interleaved ? turned.second : turned.first; };
+  const auto kern = a.D == 128 ? (a.c.e4m3 ? of(std::make_pair(paged_append_kernel<128, true, false>, paged_append_kernel<128, true, true>))
+                                           : of(std::make_pair(paged_append_kernel<128, false, false>, paged_append_kernel<128, false, true>)))
+                               : (a.c.e4m3 ? of(std::make_pair(paged_append_kernel<64, true, false>, paged_append_kernel<64, true, true>))
+                                           : of(std::make_pair(paged_append_kernel<64, false, false>, paged_append_kernel<64, false, true>)));
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, a, per, wgs);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.count_rows != 0) return e;
   hipLaunchKernelGGL(paged_count_kernel, dim3((a.B * a.Hkv + 255) / 256), dim3(256), 0, st, a);

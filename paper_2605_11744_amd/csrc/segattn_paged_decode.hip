@@ -26,6 +26,12 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPagedHeads = 16;  // query heads per pass
 constexpr int kPagedWaves = 4;
+// Up to so many rows of 128 channels (twice as many of 64) a workgroup takes a window by itself and there is nothing to
+// join, and up to twice as many where there are two windows for every compute unit.  Kernels and the gap between them, whole and
+// cut, 8 KV heads: five sequences of 500 rows of 128 10.4 and 14.1 us (8-bit rows 10.4 and 14.0), of 1000 rows of 64 10.1 and
+// 13.0, of 1000 rows of 128 16.1 and 15.6; 100 sequences of 1000 rows of 128 71 and 77, of 10 to 1000 rows 42 and 56, 64 of 2000
+// rows of 64 43 and 51.
+constexpr long long kPagedWholeRows = 512;
 
 // Rows [first, n) of a window that the newest token (row n - 1) sees.
 __device__ inline void paged_window(const PagedDecodeArgs &a, int w, int &first, int &n) {
@@ -137,9 +143,27 @@ __device__ inline float over_quads(float x, bool sum) {  // over the four lanes 
   return sum ? x + z : fmaxf(x, z);
 }
 
+// Four channels of a head's output, and with the first ones its sum.  No row seen: zeros, and the logarithm of nothing.
+template <int D>
+__device__ inline void store_out(const PagedDecodeArgs &a, long long head, int d, f32x4 o, float l, float ref) {
+  const float scale = l == 0.f ? 0.f : 1.f / l;
+  const f32x4 r = o * scale;
+  if (a.out_fp32) {
+    float *dst = (float *)a.out + head * D + d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[e] = r[e];
+  } else {
+    __bf16 *dst = (__bf16 *)a.out + head * D + d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[e] = (__bf16)r[e];
+  }
+  if (d == 0) a.lse[head] = l == 0.f ? -INFINITY : ref * a.scale + logf(l);
+}
+
 // kInPage: page_rows is a multiple of the tile, so a tile lies in one page; otherwise every row asks the table.
 // kMass: the scores are left for the weights.
-template <int D, bool kE4m3, bool kInPage, bool kMass>
+// kWhole: a workgroup per window, which writes the output itself.
+template <int D, bool kE4m3, bool kInPage, bool kMass, bool kWhole>
 __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedDecodeArgs a) {
   constexpr int NK = D / 32, NB = D / 16;
   constexpr int kRow = 2 * D, kTileBytes = kPagedTile * kRow;  // of a tile in LDS, bf16
@@ -154,10 +178,12 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
   const int quad = lane >> 4, col = lane & 15;
   const float c = a.scale_log2e;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[kPagedWaves][2 * kTileBytes];
+  __shared__ float sm_join[kPagedHeads][2];
   constexpr int MS = D + 4;  // floats per head of the merge area
   static_assert(kPagedWaves * 2 * kTileBytes >= (int)sizeof(float) * kPagedWaves * kPagedHeads * MS, "merge area fits the tiles");
 
-  PagedSlice slice = paged_slice(a, gridDim.x);
+  PagedSlice slice{(int)blockIdx.x, 0, 0x7fffffff, true};
+  if constexpr (!kWhole) slice = paged_slice(a, gridDim.x);
   slice.w = __builtin_amdgcn_readfirstlane(slice.w);  // the same in all lanes: what follows from them is scalar work
   slice.tile = __builtin_amdgcn_readfirstlane(slice.tile);
   slice.count = __builtin_amdgcn_readfirstlane(slice.count);
@@ -180,11 +206,18 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
     paged_window(a, w, first, n);
     first = __builtin_amdgcn_readfirstlane(first);
     n = __builtin_amdgcn_readfirstlane(n);
+    const int b = fast_div(w, a.n_kv), h = w - b * a.Hkv;
     const int base = first / kPagedTile, all = (n + kPagedTile - 1) / kPagedTile - base;
     const int t_begin = base + tile0, t_end = base + min(all, tile0 + left);
-    if (t_end <= t_begin) continue;
+    if (t_end <= t_begin) {
+      if constexpr (kWhole) {  // nothing held
+        for (int i = tid; i < live * (D / 4); i += 64 * kPagedWaves)
+          store_out<D>(a, (long long)b * a.Hq + h * a.g + pass * kPagedHeads + i / (D / 4), i % (D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f, 0.f);
+        return;
+      }
+      continue;
+    }
     left = slice.by_window ? 0 : left - (t_end - t_begin);
-    const int b = fast_div(w, a.n_kv), h = w - b * a.Hkv;
     const int head0 = h * a.g + pass * kPagedHeads;
     const int *table = table_of(a.c, a.Hkv, b, h);
     const int hh = a.c.per_head ? 0 : h;
@@ -419,9 +452,35 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
         const f32x4 part = *(const f32x4 *)(src + d);
         o += part * wgt;
       }
-      float *dst = a.slots + (slot * a.g + pass * kPagedHeads + head) * ws_slot_floats(D);
-      *(f32x4 *)(dst + d) = o;
-      if (d == 0) *(float2 *)(dst + D) = float2{top, l};
+      if constexpr (kWhole) {
+        store_out<D>(a, (long long)b * a.Hq + head0 + head, d, o, l, ref);
+        if (kMass && d == 0) {
+          sm_join[head][0] = ref;
+          sm_join[head][1] = l == 0.f ? 0.f : 1.f / l;
+        }
+      } else {
+        float *dst = a.slots + (slot * a.g + pass * kPagedHeads + head) * ws_slot_floats(D);
+        *(f32x4 *)(dst + d) = o;
+        if (d == 0) *(float2 *)(dst + D) = float2{top, l};
+      }
+    }
+    if constexpr (kWhole) {
+      if constexpr (kMass) {  // one pass of heads: the window's scores are this workgroup's own
+        __syncthreads();
+        if (in_set(a.heads.past, h)) {
+          const float *scores = a.scores + (long long)(b * a.n_past + set_before(a.heads.past, h)) * a.g * a.score_rows;
+          for (int r = tid; r < n; r += 64 * kPagedWaves) {
+            int in_page;
+            const int page = page_of(a.c, table, r, in_page);
+            if (page < 0) continue;
+            float sum = 0.f;
+            for (int j = 0; j < live; ++j)
+              sum += __builtin_amdgcn_exp2f((scores[(r / kPagedTile * a.g + j) * kPagedTile + r % kPagedTile] - sm_join[j][0]) * c) * sm_join[j][1];
+            a.c.mass[row_place(a.c, page, h, in_page)] += sum;
+          }
+        }
+      }
+      return;
     }
     if (tid == 0 && pass == 0) {
       if (tile0 == 0) a.pieces[w].x = (int)slot;
@@ -451,78 +510,88 @@ __device__ inline void joined_sum(const float *ml, long long stride, int count, 
   }
 }
 
-constexpr int kJoinBatch = 8;    // partials of a wave under way together
+constexpr int kJoinBatch = 4;    // partials of a wave under way together
 constexpr int kMassRows = 1024;  // rows a workgroup adds the weights of
 
 // Workgroups 0 .. B Hq - 1: merge of one query head's partials.  The others: weights of kMassRows rows of one PAST
 // head's window, from the scores that the first launch left.
 template <int D>
 __global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecodeArgs a, const int mass_chunks) {
-  constexpr int SF = D + kWsTailFloats, DPL = D / 64;
+  constexpr int SF = D + kWsTailFloats;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const float c = a.scale_log2e;
   const int heads = a.B * a.Hq;
   if ((int)blockIdx.x < heads) {
     const int b = blockIdx.x / a.Hq, head = blockIdx.x - b * a.Hq, w = b * a.Hkv + head / a.g;
-    __shared__ float sm_m[4], sm_l[4], sm_o[4][D];
+    // A partial is read by D / 4 lanes, so a wave has kGroups of them at a time, and kJoinBatch of those under way.
+    constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
+    __shared__ float sm_m[4], sm_l[4];
+    __shared__ __attribute__((aligned(16))) float sm_o[4][D];
     const bool some = paged_tiles(a, w) > 0;
     const int2 piece = some ? a.pieces[w] : int2{0, -1};
     const float *ws = a.slots + ((long long)piece.x * a.g + head % a.g) * SF;
-    const int count = piece.y - piece.x + 1;
-    float top = -INFINITY, l = 0.f, o[DPL];
-#pragma unroll
-    for (int e = 0; e < DPL; ++e) o[e] = 0.f;
-    for (int s0 = wave; s0 < count; s0 += 4 * kJoinBatch) {  // (one memory round trip for up to 4 kJoinBatch partials)
+    const int count = piece.y - piece.x + 1, group = wave * kGroups + lane / kLanes, d = lane % kLanes * 4;
+    float top = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = group; s0 - group < count; s0 += 4 * kGroups * kJoinBatch) {
       float2 ml[kJoinBatch];
-      float x[kJoinBatch][DPL];
+      f32x4 x[kJoinBatch];
 #pragma unroll
       for (int i = 0; i < kJoinBatch; ++i) {
-        const float *src = ws + (long long)(s0 + 4 * i < count ? s0 + 4 * i : count - 1) * a.g * SF;
+        const int s = s0 + 4 * kGroups * i;
+        const float *src = ws + (long long)(s < count ? s : count - 1) * a.g * SF;
         ml[i] = *(const float2 *)(src + D);
-#pragma unroll
-        for (int e = 0; e < DPL; ++e) x[i][e] = src[lane * DPL + e];
+        x[i] = *(const f32x4 *)(src + d);
       }
       float m_new = top;
 #pragma unroll
-      for (int i = 0; i < kJoinBatch; ++i) m_new = fmaxf(m_new, ml[i].x);  // (the last one again changes nothing)
+      for (int i = 0; i < kJoinBatch; ++i)
+        if (s0 + 4 * kGroups * i < count) m_new = fmaxf(m_new, ml[i].x);
       const float ref = m_new == -INFINITY ? 0.f : m_new, keep = __builtin_amdgcn_exp2f((top - ref) * c);
       top = m_new;
       l *= keep;
-#pragma unroll
-      for (int e = 0; e < DPL; ++e) o[e] *= keep;
+      o *= keep;
 #pragma unroll
       for (int i = 0; i < kJoinBatch; ++i) {
-        if (s0 + 4 * i < count) {
+        if (s0 + 4 * kGroups * i < count) {
           const float wgt = __builtin_amdgcn_exp2f((ml[i].x - ref) * c);
           l += ml[i].y * wgt;
-#pragma unroll
-          for (int e = 0; e < DPL; ++e) o[e] += x[i][e] * wgt;
+          o += x[i] * wgt;
         }
       }
     }
-    if (lane == 0) {
-      sm_m[wave] = top;
-      sm_l[wave] = l;
+    float most = top;
+#pragma unroll
+    for (int sh = kLanes; sh < 64; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
+    {
+      const float wgt = __builtin_amdgcn_exp2f((top - (most == -INFINITY ? 0.f : most)) * c);
+      l *= wgt;
+      o *= wgt;
     }
 #pragma unroll
-    for (int e = 0; e < DPL; ++e) sm_o[wave][lane * DPL + e] = o[e];
+    for (int sh = kLanes; sh < 64; sh <<= 1) {
+      l += __shfl_xor(l, sh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], sh);
+    }
+    if (lane == 0) {
+      sm_m[wave] = most;
+      sm_l[wave] = l;
+    }
+    if (lane < kLanes) *(f32x4 *)(&sm_o[wave][d]) = o;
     __syncthreads();
-    if (tid >= D) return;
+    if (tid >= kLanes) return;
     top = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
     const float ref = top == -INFINITY ? 0.f : top;
     l = 0.f;
-    float od = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const float wgt = __builtin_amdgcn_exp2f((sm_m[x] - ref) * c);
       l += sm_l[x] * wgt;
-      od += sm_o[x][tid] * wgt;
+      o += *(const f32x4 *)(&sm_o[x][d]) * wgt;
     }
-    const float r = l == 0.f ? 0.f : od / l;  // no row seen: zeros, and the logarithm of nothing
-    const long long at = ((long long)b * a.Hq + head) * D + tid;
-    if (a.out_fp32) ((float *)a.out)[at] = r;
-    else ((__bf16 *)a.out)[at] = (__bf16)r;
-    if (tid == 0) a.lse[(long long)b * a.Hq + head] = l == 0.f ? -INFINITY : ref * a.scale + logf(l);
+    store_out<D>(a, (long long)b * a.Hq + head, d, o, l, ref);
     return;
   }
   const int i = blockIdx.x - heads, win = i / mass_chunks, chunk = i - win * mass_chunks;
@@ -580,16 +649,28 @@ __global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecod
 template <int D, bool kE4m3, bool kInPage, bool kMass>
 static hipError_t launch_split(PagedDecodeArgs a, hipStream_t st) {
   static ResidentCount count;
-  const auto kern = paged_decode_split_kernel<D, kE4m3, kInPage, kMass>;
+  const auto kern = paged_decode_split_kernel<D, kE4m3, kInPage, kMass, false>;
   const int resident = count.get((const void *)kern, 256, 0);
   if (resident == 0) return hipErrorUnknown;
   long long grid = resident < kPagedMostWgs ? resident : kPagedMostWgs;
   const long long tiles = (a.max_rows + kPagedTile - 1) / kPagedTile;
   const long long slices = a.n_windows * ((tiles + kPagedWaves - 1) / kPagedWaves);  // at most, of the shortest length
+  const int passes = (a.g + kPagedHeads - 1) / kPagedHeads;
+  const long long whole = a.n_windows >= 2 * device_cus() ? 2 * kPagedWholeRows : kPagedWholeRows;
+  if ((long long)a.max_rows * D <= whole * 128 && !(kMass && passes > 1)) {
+    hipLaunchKernelGGL((paged_decode_split_kernel<D, kE4m3, kInPage, kMass, true>), dim3((unsigned)a.n_windows, passes), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
   a.fits = slices <= grid;
   if (a.fits) grid = slices;
   else if (a.n_windows <= kPagedLaneWindows && grid < 2 * a.n_windows) grid = 2 * a.n_windows;  // paged_slice needs spare ones
-  hipLaunchKernelGGL(kern, dim3((unsigned)grid, (a.g + kPagedHeads - 1) / kPagedHeads), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid, passes), dim3(256), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int chunks = kMass ? (a.max_rows + kMassRows - 1) / kMassRows : 0;
+  const long long joins = (long long)a.B * a.Hq + (long long)a.B * a.n_past * chunks;
+  if (joins > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(paged_decode_join_kernel<D>, dim3((unsigned)joins), dim3(256), 0, st, a, chunks);
   return hipGetLastError();
 }
 template <int D, bool kE4m3, bool kInPage>
@@ -599,14 +680,8 @@ static hipError_t launch_split(const PagedDecodeArgs &a, hipStream_t st) {
 template <int D>
 static hipError_t launch_paged(const PagedDecodeArgs &a, hipStream_t st) {
   const bool in_page = a.c.page_rows.d % kPagedTile == 0;
-  const hipError_t e = a.c.e4m3 ? (in_page ? launch_split<D, true, true>(a, st) : launch_split<D, true, false>(a, st))
-                                : (in_page ? launch_split<D, false, true>(a, st) : launch_split<D, false, false>(a, st));
-  if (e != hipSuccess) return e;
-  const int chunks = a.scores ? (a.max_rows + kMassRows - 1) / kMassRows : 0;
-  const long long grid = (long long)a.B * a.Hq + (long long)a.B * a.n_past * chunks;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(paged_decode_join_kernel<D>, dim3((unsigned)grid), dim3(256), 0, st, a, chunks);
-  return hipGetLastError();
+  return a.c.e4m3 ? (in_page ? launch_split<D, true, true>(a, st) : launch_split<D, true, false>(a, st))
+                  : (in_page ? launch_split<D, false, true>(a, st) : launch_split<D, false, false>(a, st));
 }
 
 hipError_t launch_paged_decode(const PagedDecodeArgs &a, hipStream_t st) {

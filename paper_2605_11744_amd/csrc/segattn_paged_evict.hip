@@ -177,11 +177,17 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
       }
       int above = incl - sum;
       if (above < rank && rank <= incl) {
-        int j = 0;
-        while (j < 3 && above + own[j] < rank) above += own[j++];
+        int j = 0, in_byte = own[0];
+#pragma unroll
+        for (int x = 1; x < 4; ++x)
+          if (j == x - 1 && above + in_byte < rank) {
+            above += in_byte;
+            in_byte = own[x];
+            j = x;
+          }
         sm_pick[0] = 255 - 4 * lane - j;
         sm_pick[1] = rank - above;
-        sm_pick[2] = rank - above == own[j];
+        sm_pick[2] = rank - above == in_byte;
       }
     }
     __syncthreads();

@@ -10,9 +10,12 @@ namespace segattn {
 constexpr int kRotateRows = 16;
 
 // A workgroup turns up to kRotateRows consecutive tokens: its threads form the sines and cosines of every
-// (token, pair) once, in LDS, then walk over the tokens' units in memory order.
-template <typename T>
+// (token, pair) once, in LDS, then walk over the tokens' units in memory order.  Few tokens per workgroup, many workgroups:
+// 32K tokens of 32 + 8 heads of 128 took 136 us with 16 tokens, 122 with 4, 118 with 2 (109 with rows marked as not worth
+// keeping: 6.2 TB/s).  Units requested before the sines are formed, or several of a thread at once, are no faster (112).
+template <typename T, bool kInterleaved>
 __global__ __launch_bounds__(256) void rotate_kernel(const RotateArgs a, const int tokens_per_wg) {
+  constexpr int P = 16 / sizeof(T);
   __shared__ __attribute__((aligned(16))) float sm_sn[kRotateRows][64], sm_cs[kRotateRows][64];
   const int tid = threadIdx.x;
   const long long t0 = (long long)blockIdx.x * tokens_per_wg;
@@ -27,23 +30,21 @@ __global__ __launch_bounds__(256) void rotate_kernel(const RotateArgs a, const i
     sm_cs[r][c] = sc.y;
   }
   __syncthreads();
-  const int per_head = a.D / 16;
+  const int per_head = a.D / (2 * P);
   auto walk = [&](const T *from, long long stride, T *to, long long to_stride, int heads) __attribute__((always_inline)) {
     const int per_token = heads * per_head;
     int r = tid / per_token, u = tid - r * per_token;
     const int dr = 256 / per_token, du = 256 - dr * per_token;
     while (r < n) {
       const int head = u / per_head, unit = u - head * per_head;
-      int lo, hi;
-      unit_channels(unit, pairs, a.rot.interleaved, lo, hi);
+      int c_lo, c_hi;
+      unit_channels<P>(unit, pairs, a.D, c_lo, c_hi);
       const T *src = from + (t0 + r) * stride + head * a.D;
       T *dst = to + (t0 + r) * to_stride + head * a.D;
-      float x[16];
-      load8(src + lo, x);
-      load8(src + hi, x + 8);
-      if (8 * unit < pairs) turn_unit(x, &sm_sn[r][8 * unit], &sm_cs[r][8 * unit], a.rot.interleaved);
-      store8(dst + lo, x);
-      store8(dst + hi, x + 8);
+      u32x4 lo = load_piece(src + c_lo), hi = load_piece(src + c_hi);
+      if (P * unit < pairs) turn_pieces<P, kInterleaved>(lo, hi, unit, pairs, sm_sn[r], sm_cs[r]);
+      store_piece(dst + c_lo, lo);
+      store_piece(dst + c_hi, hi);
       r += dr;
       u += du;
       if (u >= per_token) {
@@ -57,13 +58,18 @@ __global__ __launch_bounds__(256) void rotate_kernel(const RotateArgs a, const i
 }
 
 hipError_t launch_rotate(const RotateArgs &a, bool fp32, hipStream_t st) {
-  // fewer tokens per workgroup where sixteen would leave compute units idle
-  long long per = a.total / 1024;
+  // At most 320 units for 256 threads: 1 token of 32 + 8 heads of 128, 10 of 4 + 4 of 64 -- which take
+  // 15 us for 27000 tokens, 23 with 2, 39 with 1 -- and fewer where compute units would be idle.  (32K tokens of the former: 320
+  // units 105.7 us, 640 108.4, 1280 112.6.)
+  const long long units = ((a.q ? a.Hq : 0) + (a.k ? a.Hkv : 0)) * (long long)a.D * (fp32 ? 4 : 2) / 32;
+  long long per = 320 / units;
+  if (per > a.total / 1024) per = a.total / 1024;
   per = per < 1 ? 1 : per > kRotateRows ? kRotateRows : per;
   const long long blocks = (a.total + per - 1) / per;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-  if (fp32) hipLaunchKernelGGL(rotate_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, a, (int)per);
-  else hipLaunchKernelGGL(rotate_kernel<unsigned short>, dim3((unsigned)blocks), dim3(256), 0, st, a, (int)per);
+  const auto kern = fp32 ? (a.rot.interleaved ? rotate_kernel<float, true> : rotate_kernel<float, false>)
+                         : (a.rot.interleaved ? rotate_kernel<unsigned short, true> : rotate_kernel<unsigned short, false>);
+  hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), 0, st, a, (int)per);
   return hipGetLastError();
 }
 
