@@ -91,7 +91,7 @@ struct PagedAppendArgs {
   const int *rows;
   int *rows_out;
   int total, B, Hq, Hkv, D;
-  int count_rows;         // the token kernel also writes rows_out: 1 each workgroup its sequence's, 2 a workgroup behind the others
+  int count_rows;         // the token kernel also writes rows_out: 1 each workgroup its sequence's, 2 workgroups behind the others
 };
 
 // ---- decode -----------------------------------------------------------------------------------

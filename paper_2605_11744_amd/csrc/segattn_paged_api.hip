@@ -130,7 +130,7 @@ bool decode_space(const Problem &p, const PagedCache &c, int64_t max_rows, int a
   if (windows * ((max_rows + kPagedTile - 1) / kPagedTile + 1) >= (1ull << 31)) return false;
   s.pieces = 0;
   s.slots = align_up(windows * 8ull);
-  s.scores = align_up(s.slots + (kPagedMostWgs + windows) * p.g * ws_slot_floats(p.D) * 4ull);
+  s.scores = align_up(s.slots + (kPagedMostWgs + windows + 256) * p.g * ws_slot_floats(p.D) * 4ull);
   s.score_rows = accumulate ? (max_rows + kPagedTile - 1) / kPagedTile * kPagedTile : 0;
   s.total = s.scores + align_up((unsigned long long)p.B * p.n_past * p.g * s.score_rows * 4ull);
   return s.total < (1ull << 46);

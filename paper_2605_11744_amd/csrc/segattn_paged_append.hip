@@ -40,6 +40,15 @@ __device__ inline uint2 e4m3_of(const float *x, float inverse) {
   return uint2{(unsigned)a, (unsigned)b};
 }
 
+// The new row count of window w = b * Hkv + h.
+__device__ inline void count_rows(const PagedAppendArgs &a, int w) {
+  if (w >= a.B * a.Hkv) return;
+  const int b = w / a.Hkv;
+  const long long held = rows_held(a.rows, w, a.c.cap);
+  const long long sum = held + (a.cu ? a.cu[b + 1] - a.cu[b] : 1);
+  a.rows_out[w] = sum < held ? (int)held : sum < a.c.cap ? (int)sum : a.c.cap;
+}
+
 // A workgroup takes up to kAppendRows consecutive tokens.  First it finds every token's sequence and every
 // (token, head)'s row, and forms the sines, in LDS; then its threads walk over the units of the queries, the
 // keys and the values.  The D / 16 threads of a row are neighbours in one wave, which finds an e4m3 row's
@@ -51,13 +60,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedAppendArgs
   __shared__ int sm_seq[kAppendRows], sm_index[kAppendRows];
   __shared__ int2 sm_row[kAppendRows * kMaxKvHeads];  // page (or -1) and row in it
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  if ((int)blockIdx.x >= token_wgs) {  // the new row counts
-    for (int w = tid; w < a.B * a.Hkv; w += 256) {
-      const int b = w / a.Hkv;
-      const long long held = rows_held(a.rows, w, a.c.cap);
-      const long long sum = held + (a.cu ? a.cu[b + 1] - a.cu[b] : 1);
-      a.rows_out[w] = sum < held ? (int)held : sum < a.c.cap ? (int)sum : a.c.cap;
-    }
+  if ((int)blockIdx.x >= token_wgs) {
+    count_rows(a, ((int)blockIdx.x - token_wgs) * 256 + tid);
     return;
   }
   const int t0 = (int)blockIdx.x * tokens_per_wg;
@@ -169,12 +173,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedAppendArgs
 }
 
 __global__ __launch_bounds__(256) void paged_count_kernel(const PagedAppendArgs a) {
-  const int w = blockIdx.x * 256 + threadIdx.x;
-  if (w >= a.B * a.Hkv) return;
-  const int b = w / a.Hkv;
-  const long long held = rows_held(a.rows, w, a.c.cap);
-  const long long sum = held + (a.cu ? a.cu[b + 1] - a.cu[b] : 1);
-  a.rows_out[w] = sum < held ? (int)held : sum < a.c.cap ? (int)sum : a.c.cap;
+  count_rows(a, blockIdx.x * 256 + threadIdx.x);
 }
 
 hipError_t launch_paged_append(const PagedAppendArgs &args, hipStream_t st) {
@@ -186,7 +185,7 @@ hipError_t launch_paged_append(const PagedAppendArgs &args, hipStream_t st) {
   // own workgroup where a sequence has one token, else by a launch of its own.
   const bool in_place = a.rows == a.rows_out;
   a.count_rows = !in_place ? 2 : (a.cu == nullptr && per == 1) ? 1 : 0;
-  const int grid = wgs + (a.count_rows == 2 ? 1 : 0);
+  const int count_wgs = (a.B * a.Hkv + 255) / 256, grid = wgs + (a.count_rows == 2 ? count_wgs : 0);
   const auto of = [&](auto turned) { return a.rot.interleaved ? turned.second : turned.first; };
   const auto kern = a.D == 128 ? (a.c.e4m3 ? of(std::make_pair(paged_append_kernel<128, true, false>, paged_append_kernel<128, true, true>))
                                            : of(std::make_pair(paged_append_kernel<128, false, false>, paged_append_kernel<128, false, true>)))
@@ -195,7 +194,7 @@ hipError_t launch_paged_append(const PagedAppendArgs &args, hipStream_t st) {
   hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, a, per, wgs);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.count_rows != 0) return e;
-  hipLaunchKernelGGL(paged_count_kernel, dim3((a.B * a.Hkv + 255) / 256), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(paged_count_kernel, dim3(count_wgs), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

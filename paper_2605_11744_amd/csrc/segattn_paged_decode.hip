@@ -50,16 +50,18 @@ __device__ inline int paged_tiles(const PagedDecodeArgs &a, int w) {
 }
 
 // This workgroup's slice: tiles [tile, tile + count) counted from window w's first one; a count that goes beyond the
-// window goes on in the next ones (not in the first form).  Every slice is a multiple of one tile per wave.
+// window goes on in the next ones (not in the first form).  Every slice is a multiple of one tile per wave.  The
+// first form is in the order of their numbers; the second one's order (next_window) is that of its search.
 struct PagedSlice {
   int w, tile, count;
   bool by_window;
+  int order;  // w's place in the order
 };
 __device__ inline PagedSlice paged_slice(const PagedDecodeArgs &a, int wgs) {
   const int lane = threadIdx.x & 63, me = blockIdx.x;
   constexpr int kLeast = kPagedWaves;
   auto whole = [](int tiles) { return (tiles + kPagedWaves - 1) / kPagedWaves * kPagedWaves; };
-  PagedSlice s{-1, 0, 0, true};
+  PagedSlice s{-1, 0, 0, true, 0};
   if (a.n_windows <= kPagedLaneWindows) {
     // Few windows: each is cut by itself, into slices as long as the grid needs them, a lane per window.
     const int tiles = lane < a.n_windows ? paged_tiles(a, lane) : 0;
@@ -86,13 +88,14 @@ __device__ inline PagedSlice paged_slice(const PagedDecodeArgs &a, int wgs) {
     s.count = count;
     return s;
   }
-  // Many windows: all tiles end to end, cut evenly.  A thread adds up a run of consecutive windows, every wave scans
-  // the 256 sums, four a lane, and walks the run that holds the slice's first tile.
+  // Many windows: all tiles end to end, cut evenly.  A thread adds up the windows tid, tid + 256, ... (so that neighbours read
+  // neighbouring counts), every wave scans the 256 sums, four a lane, and walks the windows of the one that holds the
+  // slice's first tile.
   __shared__ __attribute__((aligned(16))) int sm_run[256];
   const int tid = threadIdx.x, run = (a.n_windows + 255) / 256;
   int sum = 0;
   for (int j = 0; j < run; ++j)
-    if (tid * run + j < a.n_windows) sum += paged_tiles(a, tid * run + j);
+    if (j * 256 + tid < a.n_windows) sum += paged_tiles(a, j * 256 + tid);
   sm_run[tid] = sum;
   __syncthreads();
   int part[4], incl = 0;
@@ -122,18 +125,29 @@ __device__ inline PagedSlice paged_slice(const PagedDecodeArgs &a, int wgs) {
       ++t;
     }
   }
-  int w = t * run;
-  for (int j = 0; j + 1 < run; ++j) {
+  int w = t;  // the window that holds the tile: below n_windows, since those behind have no tiles
+  for (; w + 256 < a.n_windows; w += 256) {
     const int n = paged_tiles(a, w);
     if (before + n > start) break;
     before += n;
-    ++w;
   }
   s.w = __builtin_amdgcn_readfirstlane(w);
+  s.order = t * run + s.w / 256;
   s.tile = __builtin_amdgcn_readfirstlane(start - before);
   s.count = count;
   s.by_window = false;
   return s;
+}
+
+// The window behind w in the order of the second form; n_windows or above: none.  It skips no window, and a step of the
+// order per call (places of the order without a window included) numbers the slots.
+__device__ inline int next_window(const PagedDecodeArgs &a, int w, int &order) {
+  const int run = (a.n_windows + 255) / 256;
+  ++order;
+  if (w + 256 < a.n_windows) return w + 256;
+  const int t = (w & 255) + 1;
+  order = t * run;
+  return t < 256 ? t : a.n_windows;
 }
 
 __device__ inline float over_quads(float x, bool sum) {  // over the four lanes of a column
@@ -182,7 +196,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
   constexpr int MS = D + 4;  // floats per head of the merge area
   static_assert(kPagedWaves * 2 * kTileBytes >= (int)sizeof(float) * kPagedWaves * kPagedHeads * MS, "merge area fits the tiles");
 
-  PagedSlice slice{(int)blockIdx.x, 0, 0x7fffffff, true};
+  PagedSlice slice{(int)blockIdx.x, 0, 0x7fffffff, true, 0};
   if constexpr (!kWhole) slice = paged_slice(a, gridDim.x);
   slice.w = __builtin_amdgcn_readfirstlane(slice.w);  // the same in all lanes: what follows from them is scalar work
   slice.tile = __builtin_amdgcn_readfirstlane(slice.tile);
@@ -201,7 +215,8 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
     voff[nb] = kTileBytes + vrow * kRow + (chunk_v(vrow, 2 * nb + ((col & 3) >> 1)) << 4) + 8 * (col & 1);
 
   int left = slice.count;
-  for (int w = slice.w, tile0 = slice.tile; left > 0 && w < a.n_windows; ++w, tile0 = 0) {
+  int order = __builtin_amdgcn_readfirstlane(slice.order);
+  for (int w = slice.w, tile0 = slice.tile; left > 0 && w < a.n_windows; w = next_window(a, w, order), tile0 = 0) {
     int first, n;
     paged_window(a, w, first, n);
     first = __builtin_amdgcn_readfirstlane(first);
@@ -434,7 +449,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
       }
     }
     __syncthreads();
-    const long long slot = blockIdx.x + (slice.by_window ? 0 : w);
+    const long long slot = blockIdx.x + (slice.by_window ? 0 : order);  // one more with the workgroup, the window or both
     for (int i = tid; i < live * (D / 4); i += 64 * kPagedWaves) {
       const int head = i / (D / 4), d = (i % (D / 4)) * 4;
       float top = -INFINITY;

@@ -283,6 +283,53 @@ def test_decode_of_hundreds_of_windows():
     _decode(pool, 4, lengths, accumulate=True)
 
 
+@pytest.mark.parametrize("batch,hkv", [(300, 1), (90, 6), (65, 1), (257, 1), (128, 2)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_decode_of_hundreds_of_windows_cut_evenly(batch, hkv, accumulate):
+    """Room for rows that a workgroup would not take by itself, held by one sequence only: windows of every length, empty
+    ones among them, shared out evenly; over 256 of them a thread of the search has more than one."""
+    lengths = [[(7919 * (i + 3) * (h + 1)) % 130 * (i % 5 > 0) for h in range(hkv)] for i in range(batch)]
+    lengths[batch // 2] = [1111] * hkv
+    pool = Pool(batch=batch, hkv=hkv, d=128, page_rows=32, max_pages=35, spare=0)
+    pool.fill(lengths)
+    _decode(pool, 2 * hkv, lengths, accumulate=accumulate, policy=[2 + h % 2 for h in range(hkv)])
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=lambda k: "-".join(f"{a}{b}" for a, b in k.items()))
+@pytest.mark.parametrize("d,g,batch", [(128, 4, 7), (64, 3, 7), (64, 1, 40)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_decode_of_ragged_lengths_in_a_roomy_table(kind, d, g, batch, accumulate):
+    """The same lengths where the table has room for thousands of rows: windows are cut and joined."""
+    lengths = [0, 1, 31, 32, 33, 129, 517]
+    lengths = [lengths[i % 7] for i in range(batch)]
+    pool = Pool(batch=batch, hkv=2, d=d, max_pages=-(-520 // kind["page_rows"]), **kind).fill(lengths)
+    room = -(-4200 // kind["page_rows"])
+    table = torch.full((*pool.table.shape[:-1], room), -1, dtype=torch.int32, device="cuda")
+    table[..., :pool.max_pages] = pool.table
+    pool.table, pool.max_pages = table, room
+    _decode(pool, 2 * g, lengths, accumulate=accumulate)
+
+
+def test_counts_of_many_sequences():
+    """More (sequence, head) pairs than a workgroup has threads, in and out of place."""
+    B = 700
+    pool = Pool(batch=B, hkv=3, d=64, page_rows=4, max_pages=1, mass=False, pos=False)
+    pool.rows.copy_((torch.arange(B * 3, dtype=torch.int32, device="cuda") % 5).view(B, 3))
+    m = [i % 4 for i in range(B)]
+    cu = torch.tensor([sum(m[:i]) for i in range(B + 1)], dtype=torch.int32, device="cuda")
+    n = int(cu[-1])
+    k = torch.ones((n, 3, 64), dtype=BF16, device="cuda")
+    want = (pool.rows + torch.tensor(m, device="cuda")[:, None]).clamp(max=4).to(torch.int32)
+    out = torch.empty_like(pool.rows)
+    sa.seg_kv_paged_append(_cfg(pool, 3), pool.pages(), None, None, k, k, cu, n, 3, None, pool.rows, None, out, _stream())
+    assert torch.equal(out, want)
+    sa.seg_kv_paged_append(_cfg(pool, 3), pool.pages(), None, None, k, k, cu, n, 3, None, pool.rows, None, pool.rows, _stream())
+    assert torch.equal(pool.rows, want)
+    k = torch.ones((B, 3, 64), dtype=BF16, device="cuda")
+    sa.seg_kv_paged_append(_cfg(pool, 3), pool.pages(), None, None, k, k, None, B, 1, None, pool.rows, None, pool.rows, _stream())
+    assert torch.equal(pool.rows, (want + 1).clamp(max=4).to(torch.int32))
+
+
 @pytest.mark.parametrize("batch,lengths", [(1, [40000]), (3, [9000, 70, 16385])])
 @pytest.mark.parametrize("kind", [dict(page_rows=64), dict(page_rows=48, e4m3=True)], ids=["bf16", "e4m3"])
 def test_decode_of_long_caches(batch, lengths, kind):
