@@ -81,6 +81,7 @@ bool build_pages(const segattn_pages *g, const Problem &p, PagedCache &c) {
   if (g->per_head) head = 0;
   else if ((heads > 1 && head < 1) || head < 0 || head >= (1ll << 40) || head * size % 16) return false;
   if (page == 0 && g->n_pages > 1) return false;
+  if ((double)g->n_pages * page * size > 4e18) return false;
   if (misaligned(g->k, 16) || misaligned(g->v, 16) || misaligned(g->table, 4) || misaligned(g->mass, 4) || misaligned(g->pos, 4)) return false;
   if (g->type == SEGATTN_PAGES_E4M3 && (!g->k_scale || !g->v_scale)) return false;
   memset(&c, 0, sizeof(c));

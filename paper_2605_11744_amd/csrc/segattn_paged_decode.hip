@@ -27,10 +27,11 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kPagedHeads = 16;  // query heads per pass
 constexpr int kPagedWaves = 4;
 // Up to so many rows of 128 channels (twice as many of 64) a workgroup takes a window by itself and there is nothing to
-// join, and up to twice as many where there are two windows for every compute unit.  Kernels and the gap between them, whole and
-// cut, 8 KV heads: five sequences of 500 rows of 128 10.4 and 14.1 us (8-bit rows 10.4 and 14.0), of 1000 rows of 64 10.1 and
-// 13.0, of 1000 rows of 128 16.1 and 15.6; 100 sequences of 1000 rows of 128 71 and 77, of 10 to 1000 rows 42 and 56, 64 of 2000
-// rows of 64 43 and 51.
+// join; times the windows per compute unit, up to eight, since a window that is longer than the others then weighs less.
+// Kernels and the gap between them, whole and cut, 8 KV heads: five sequences of 500 rows of 128 10.4 and 14.1 us (8-bit rows
+// 10.4 and 14.0), of 1000 rows of 64 10.1 and 13.0, of 1000 rows of 128 16.1 and 15.6; 100 sequences of 10 to 1000 rows of 128 42
+// and 56, 128 of 100 to 2000 98 and 105, 500 of 1100 to 3000 662 and 712.  (64 of 2000 to 4000: 131 and 135, but one long
+// window among short ones would be waited for.)
 constexpr long long kPagedWholeRows = 512;
 
 // Rows [first, n) of a window that the newest token (row n - 1) sees.
@@ -671,7 +672,7 @@ static hipError_t launch_split(PagedDecodeArgs a, hipStream_t st) {
   const long long tiles = (a.max_rows + kPagedTile - 1) / kPagedTile;
   const long long slices = a.n_windows * ((tiles + kPagedWaves - 1) / kPagedWaves);  // at most, of the shortest length
   const int passes = (a.g + kPagedHeads - 1) / kPagedHeads;
-  const long long whole = a.n_windows >= 2 * device_cus() ? 2 * kPagedWholeRows : kPagedWholeRows;
+  const long long per_cu = a.n_windows / device_cus(), whole = kPagedWholeRows * (per_cu < 1 ? 1 : per_cu > 8 ? 8 : per_cu);
   if ((long long)a.max_rows * D <= whole * 128 && !(kMass && passes > 1)) {
     hipLaunchKernelGGL((paged_decode_split_kernel<D, kE4m3, kInPage, kMass, true>), dim3((unsigned)a.n_windows, passes), dim3(256), 0, st, a);
     return hipGetLastError();

@@ -468,6 +468,30 @@ def test_eviction_of_a_table_with_holes_and_of_a_promise():
     _evict(pool, 10 ** 12, 10 ** 11, 2)
 
 
+def test_pools_beyond_32_bits_of_offset():
+    """600,000 pages of 16 KB: the same sequences in a small pool and in a large one, through append, decode and eviction."""
+    small, large = (Pool(batch=2, hkv=2, d=128, page_rows=64, max_pages=12, per_head=True, spare=n, seed=n).fill([500, 700]) for n in (0, 600000))
+    assert int(large.table.max()) * large.k.stride(0) * 2 > 2 ** 32
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn((2, h, 128), generator=g).to(BF16).cuda() for h in (8, 2, 2))
+    for pool in (small, large):
+        sa.seg_kv_paged_append(_cfg(pool, 8), pool.pages(), None, None, k, v, None, 2, 1, torch.tensor([500, 700], device="cuda"), pool.rows, None,
+                               pool.rows, _stream())
+        _decode(pool, 8, [501, 701], q=q, accumulate=True)
+    cfg = _cfg(small, 2)
+    for pool in (small, large):
+        need = sa.seg_kv_paged_evict_workspace_bytes(cfg, pool.pages(), 768, 300)
+        sa.seg_kv_paged_evict(cfg, pool.pages(), pool.rows, 768, 300, 30, 4, pool.rows, torch.empty(need, dtype=torch.uint8, device="cuda"), need, _stream())
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(2):
+            for x, y in zip(small.kv(b, h, range(300)), large.kv(b, h, range(300))):
+                assert torch.equal(x, y)
+            for name in ("mass", "pos"):
+                x, y = (getattr(p, name)[p.place(b, h, range(300))[0].cuda(), 0, (torch.arange(300) % 64).cuda()] for p in (small, large))
+                assert torch.equal(x, y), name
+
+
 # ---- together --------------------------------------------------------------------------------------
 def test_prompt_then_steps_that_accumulate_then_evict():
     """A program's loop: prompt appended turned, steps of append and decode that add up weights, an eviction every

@@ -66,7 +66,8 @@ BAD_PAGES = [
     dict(row_stride=64, head_stride=4096, page_stride=8192), dict(row_stride=132, head_stride=8192, page_stride=16384),
     dict(row_stride=128, head_stride=4100, page_stride=8192), dict(row_stride=128, head_stride=4096, page_stride=0),
     dict(row_stride=128, head_stride=0, page_stride=8192), dict(row_stride=128, head_stride=-4096, page_stride=8192),
-    dict(mass=P + 2), dict(pos=P + 1),
+    dict(mass=P + 2), dict(pos=P + 1), dict(row_stride=128, head_stride=4096, page_stride=1 << 40),
+    dict(row_stride=128, head_stride=4096, page_stride=1 << 39, n_pages=1 << 30),
 ]
 
 
