@@ -22,7 +22,8 @@ constexpr int kCopies = 4;        // of the histogram: neighbouring lanes count 
 constexpr int kAtOnce = 4;        // rows of a lane that are under way together
 
 // The select kernel walks over a window's keys seven times, so they are formed once (a key costs a look into the
-// table and two loads) and kept: in LDS (kHeld), or for longer windows in the workspace.  Wave x has a run of consecutive
+// table and two loads) and kept: in LDS (kHeld; the positions in registers until the newest is known), or for longer windows in
+// the workspace.  Wave x has a run of consecutive
 // rows, 64 at a time.  The histogram is kept kCopies times: weights share few exponents, and 64 lanes that count
 // the same byte in one word wait for each other.
 //
@@ -88,10 +89,9 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
     }
   };
   const int beside = kInPage ? lane : 0;  // (a page has room for all 64 rows, also behind the last one)
-  for (int r = r0; r < r0 + run; r += 64 * kAtOnce) {
+  auto form_weights = [&](int r, int (&pos)[kAtOnce]) __attribute__((always_inline)) {  // positions: kNowhere for a row without one
     ask(r);
     find(r);
-    int pos[kAtOnce];
     float mass[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
@@ -102,8 +102,20 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
     for (int i = 0; i < kAtOnce; ++i) {
       const bool held = place[i] >= 0 && r + 64 * i + lane < r1;
       if (r + 64 * i < r0 + run) keys[r + 64 * i + lane] = held && mass[i] > 0.f ? __float_as_uint(mass[i]) : 0u;
-      if (held && pos[i] > newest) newest = pos[i];
+      if (!held) pos[i] = kNowhere;
+      newest = pos[i] > newest ? pos[i] : newest;
     }
+  };
+  constexpr int kBatches = kHeldRows / kSelectThreads / kAtOnce;  // of a wave's rows, where their keys fit LDS
+  int kept_pos[kHeld ? kBatches : 1][kAtOnce];
+  if constexpr (kHeld) {
+#pragma unroll
+    for (int y = 0; y < kBatches; ++y) {
+      if (64 * kAtOnce * y >= run) break;
+      form_weights(r0 + 64 * kAtOnce * y, kept_pos[y]);
+    }
+  } else {
+    for (int r = r0; r < r0 + run; r += 64 * kAtOnce) form_weights(r, kept_pos[0]);
   }
 #pragma unroll
   for (int sh = 1; sh < 64; sh <<= 1) {
@@ -118,15 +130,27 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
   // positions above newest - recent stay, as a bound that an int holds
   const int above = (long long)newest - a.recent < kNowhere ? kNowhere : newest - a.recent;
   const int from = a.first > 0 ? a.first : kNowhere;
-  for (int r = r0; r < r1; r += 64 * kAtOnce) {
-    if (run > 64 * 64) ask(r);
-    find(r);
-    int pos[kAtOnce];
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) pos[i] = (a.c.pos + (place[i] < 0 ? 0 : place[i]))[place[i] < 0 ? 0 : beside];
+  auto sure = [&](int r, const int (&pos)[kAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i)
-      if (place[i] >= 0 && (pos[i] > above || pos[i] < from) && r + 64 * i + lane < r1) keys[r + 64 * i + lane] = kSureKey;
+      if ((pos[i] > above || pos[i] < from) && pos[i] != kNowhere) keys[r + 64 * i + lane] = kSureKey;
+  };
+  if constexpr (kHeld) {
+#pragma unroll
+    for (int y = 0; y < kBatches; ++y) {
+      if (64 * kAtOnce * y >= run) break;
+      sure(r0 + 64 * kAtOnce * y, kept_pos[y]);
+    }
+  } else {
+    for (int r = r0; r < r1; r += 64 * kAtOnce) {
+      int pos[kAtOnce];
+      if (run > 64 * 64) ask(r);
+      find(r);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        pos[i] = place[i] >= 0 && r + 64 * i + lane < r1 ? (a.c.pos + place[i])[beside] : kNowhere;
+      sure(r, pos);
+    }
   }
   // (a wave reads only the keys that it wrote itself: no barrier)
   // body(row of lane 0, key) for 64 rows at a time, in order.  The rows from n on have the lowest key, and being the last
