@@ -185,9 +185,10 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
   constexpr int kPieces = (kE4m3 ? D : 2 * D) / 16;            // 16-byte pieces of a row in memory
   constexpr int RPL = 64 / kPieces, NL = kPagedTile / RPL;     // rows per wave load, loads per tile and tensor
   // Where a row's 16-byte chunk lies: XORed so that 16 rows read at one chunk (K), or 8 rows at two (V), meet every bank once,
-  // and so do the eight lanes that write every other chunk of an 8-bit row (its upper half is flipped against the lower one).
-  auto chunk_k = [](int row, int chunk) { return D == 128 ? chunk ^ (chunk >> 3) ^ (row & 15) : chunk ^ ((row >> 1) & 7); };
-  auto chunk_v = [](int row, int chunk) { return D == 128 ? chunk ^ (chunk >> 3) ^ (2 * (row & 7)) : chunk ^ (2 * ((row >> 1) & 3)); };
+  // and so do the eight lanes that write every other chunk of an 8-bit row, whose upper half is flipped against the lower one,
+  // or (D = 64) of two rows, the odd one flipped.
+  auto chunk_k = [](int row, int chunk) { return D == 128 ? chunk ^ (chunk >> 3) ^ (row & 15) : chunk ^ ((row >> 1) & 7) ^ (row & 1); };
+  auto chunk_v = [](int row, int chunk) { return D == 128 ? chunk ^ (chunk >> 3) ^ (2 * (row & 7)) : chunk ^ (2 * ((row >> 1) & 3)) ^ (row & 1); };
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int quad = lane >> 4, col = lane & 15;
