@@ -198,7 +198,7 @@ typedef struct {
                             scaling (copied)                                                         */
 } segattn_rope;
 
-/* Turns q [B*rows,Hq,D] and k [B*rows,Hkv,D] into q_out and k_out (either pair may be NULL; in place where the
+/* Turns q [B*rows,Hq,D] and k [B*rows,Hkv,D] (B * rows < 2^31 - 4096) into q_out and k_out (either pair may be NULL; in place where the
  * pointers are the same).  Row t of sequence b is at position pos0[b] + t (device int64 [B]; NULL: all 0), or row
  * j of all at pos[j] (device int64 [B*rows]: packed batches, caches that were evicted from; not both).  The
  * strides are in elements between token rows, 0 for dense, so that q and k can be parts of one projection's
@@ -457,7 +457,7 @@ typedef struct {
  * (device int32 [B+1], ascending from 0; max_seqlen: the most of one sequence, total: all, host values), or NULL
  * for one token per sequence (total = B, max_seqlen = 1).  They become rows rows[b,h] on of every KV head, and
  * rows_out[b,h] = rows[b,h] + their number (rows_out may be rows).  Token i of a sequence is at position
- * pos0[b] + i (device int64 [B]; NULL: all 0), which pos gets and, with a rope, the key is turned by; q
+ * pos0[b] + i (device int64 [B]; NULL: all 0; below 2^31), which pos gets and, with a rope, the key is turned by; q
  * [total,Hq,D] (NULL: none) is then turned into q_out (may be q).  Without a rope keys are taken as they are
  * (and q is not needed).  mass, where there is one, starts at 0.  e4m3: a row is stored with the smallest
  * power of two 2^e >= 2^-119 for which its largest finite magnitude is at most 448 * 2^e, every element rounded

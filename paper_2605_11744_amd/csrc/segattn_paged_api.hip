@@ -173,7 +173,7 @@ segattn_status seg_rope_rotate(const segattn_config *cfg, const segattn_rope *ro
   memset(&a, 0, sizeof(a));
   if (!build_rotary(rope, p.D, a.rot)) return SEGATTN_EINVAL;
   if ((!q && !k) || (q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return SEGATTN_EINVAL;
-  if (rows < 1 || rows >= kMostRows || (long long)p.B * rows >= (1ll << 40) || (pos0 && pos)) return SEGATTN_EINVAL;
+  if (rows < 1 || rows >= kMostRows || (long long)p.B * rows >= kMostRows || (pos0 && pos)) return SEGATTN_EINVAL;
   if (inverse < 0 || inverse > 1 || fp32 < 0 || fp32 > 1) return SEGATTN_EINVAL;
   const long long of_q = (long long)p.Hq * p.D, of_k = (long long)p.Hkv * p.D, size = fp32 ? 4 : 2;
   struct {

@@ -8,7 +8,8 @@
 //
 // select: one workgroup per window finds the key of rank `keep` by counting, a byte of the key at a time, then lists
 // the free places and the rows that go there.  move: copies them, many workgroups per window.  Bound by the
-// bytes of the moved rows where many move, else by the passes over the keys.
+// bytes of the moved rows where many move, else by the passes over the keys: 96 windows of up to 32768 rows to 16384, 44 us
+// for the selection and 89 for 0.38 GB of moves (4.3 TB/s); 32 windows of 1100 to 1279 rows to 1024, 10 and 4.5.
 #include "segattn_paged.h"
 
 namespace segattn {
@@ -18,14 +19,14 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr unsigned kSureKey = 0xffffffffu;
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kHeldRows = 32 * kSelectThreads;  // rows whose keys fit the select kernel's LDS
-constexpr int kCopies = 4;        // of the histogram: neighbouring lanes count in different ones
-constexpr int kAtOnce = 4;        // rows of a lane that are under way together
+constexpr int kCopies = 4;  // of the histogram: neighbouring lanes count in different ones
+constexpr int kAtOnce = 4;  // rows of a lane that are under way together
 
 // The select kernel walks over a window's keys seven times, so they are formed once (a key costs a look into the
 // table and two loads) and kept: in LDS (kHeld; the positions in registers until the newest is known), or for longer windows in
-// the workspace.  Wave x has a run of consecutive
-// rows, 64 at a time.  The histogram is kept kCopies times: weights share few exponents, and 64 lanes that count
-// the same byte in one word wait for each other.
+// the workspace.  Wave x has a run of consecutive rows, 64 at a time.  The histogram is kept kCopies times: weights share
+// few exponents, protected rows all bits, and lanes that count the same byte in one word wait for each other.  (Of 11 bits at
+// a time, in one copy: 5.5K rows, 901 of them protected, 18.3 us instead of 17.1.)
 //
 // One compute unit works on a window, and a vector instruction more per 64 rows is 0.25 us more for 32768.  kInPage:
 // page_rows is a multiple of 64, so 64 rows lie in one page and are found with scalar instructions.
