@@ -147,7 +147,7 @@ bool evict_space(const Problem &p, const PagedCache &c, int64_t max_rows, int64_
   s.most_moves = max_rows <= keep ? 0 : max_rows - keep < keep ? max_rows - keep : keep;
   const unsigned long long windows = (unsigned long long)p.B * p.Hkv;
   s.lists = align_up(windows * 4ull);
-  s.keys = align_up(s.lists + windows * 2ull * s.most_moves * 4ull);
+  s.keys = align_up(s.lists + windows * 2ull * s.most_moves * 8ull);
   s.key_rows = s.most_moves == 0 || evict_keys_held(max_rows) ? 0 : (max_rows + 1023) / 1024 * 1024;
   s.total = s.keys + align_up(windows * 4ull * s.key_rows);
   return s.total < (1ull << 46);
@@ -315,7 +315,7 @@ segattn_status seg_kv_paged_evict(const segattn_config *cfg, const segattn_pages
   a.rows = rows;
   a.rows_out = rows_out;
   a.moves = (int *)ws;
-  a.lists = (int *)(ws + s.lists);
+  a.lists = (int2 *)(ws + s.lists);
   a.keys = s.key_rows ? (unsigned *)(ws + s.keys) : nullptr;
   a.key_rows = s.key_rows;
   fill_heads(p, a.heads);

@@ -8,8 +8,8 @@
 //
 // select: one workgroup per window finds the key of rank `keep` by counting, a byte of the key at a time, then lists
 // the free places and the rows that go there.  move: copies them, many workgroups per window.  Bound by the
-// bytes of the moved rows where many move, else by the passes over the keys: 96 windows of up to 32768 rows to 16384, 44 us
-// for the selection and 89 for 0.38 GB of moves (4.3 TB/s); 32 windows of 1100 to 1279 rows to 1024, 10 and 4.5.
+// bytes of the moved rows where many move, else by the passes over the keys: 96 windows of up to 32768 rows to 16384, 46 us
+// for the selection and 82 for 0.38 GB of moves (4.6 TB/s); 32 windows of 1100 to 1279 rows to 1024, 9.9 and 3.9.
 #include "segattn_paged.h"
 
 namespace segattn {
@@ -262,7 +262,17 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
   auto before = [](unsigned long long m) __attribute__((always_inline)) {  // set bits of lanes below this one
     return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u));
   };
-  int *place_list = a.lists + (long long)w * 2 * a.most_moves, *mover_list = place_list + a.most_moves;
+  int2 *place_list = a.lists + (long long)w * 2 * a.most_moves, *mover_list = place_list + a.most_moves;
+  auto found = [&](int r) __attribute__((always_inline)) {  // row r + lane
+    int2 at;
+    if constexpr (kInPage) {
+      at.x = __builtin_amdgcn_readlane(entry, ((r - r0) >> 6) & 63);
+      at.y = r - fast_div(r, a.c.page_rows) * (int)a.c.page_rows.d + lane;
+    } else {
+      at.x = page_of(a.c, table, r + lane < n ? r + lane : n - 1, at.y);
+    }
+    return at;
+  };
   over_rows([&](int r, unsigned key) __attribute__((always_inline)) {
     unsigned long long stays = __builtin_amdgcn_ballot_w64(key > edge);
     const unsigned long long tie = __builtin_amdgcn_ballot_w64(key == edge);
@@ -272,70 +282,65 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
     }
     const unsigned long long lo = r + 64 <= a.keep ? ~0ull : r >= a.keep ? 0ull : (1ull << (a.keep - r)) - 1;
     const unsigned long long pm = ~stays & lo, mm = stays & ~lo;
+    if (kInPage && run > 64 * 64) ask(r);
     if (pm) {
       const int i = places + before(pm);
-      if (((pm >> lane) & 1) && i < a.most_moves) place_list[i] = r + lane;
+      const int2 at = found(r);
+      if (((pm >> lane) & 1) && i < a.most_moves) place_list[i] = at;
       places += __popcll(pm);
     }
     if (mm) {
       const int i = movers + before(mm);
-      if (((mm >> lane) & 1) && i < a.most_moves) mover_list[i] = r + lane;
+      const int2 at = found(r);
+      if (((mm >> lane) & 1) && i < a.most_moves) mover_list[i] = at;
       movers += __popcll(mm);
     }
   });
 }
 
 // Rows of keys and values (2 D bytes each, D as e4m3), 16 bytes a lane; kMovesAtOnce rows of a lane are under way
-// together, since each is a chain of three accesses: lists, table, row.
+// together, since each is a chain of accesses: lists, row.  The lists hold pages, which the select kernel has at hand: with row
+// numbers in them, looked up in the table here, 12 prompts of 2.4K to 14K rows took 137 us instead of 133.
 constexpr int kMovesAtOnce = 4;
 __global__ __launch_bounds__(256) void paged_move_kernel(const PagedEvictArgs a) {
   const int w = blockIdx.x, b = w / a.Hkv, h = w - b * a.Hkv;
   const int count = a.moves[w];
   const int pieces = (a.c.e4m3 ? a.D : 2 * a.D) / 16, per = 256 / (2 * pieces);  // lanes per tensor, rows at a time
   const int piece = threadIdx.x % pieces, is_v = (threadIdx.x / pieces) & 1, mine = threadIdx.x / (2 * pieces);
-  const int *table = table_of(a.c, a.Hkv, b, h);
-  const int *place_list = a.lists + (long long)w * 2 * a.most_moves, *mover_list = place_list + a.most_moves;
+  const int2 *place_list = a.lists + (long long)w * 2 * a.most_moves, *mover_list = place_list + a.most_moves;
   unsigned char *pool = is_v ? a.c.v : a.c.k;
   unsigned char *scale = is_v ? a.c.v_scale : a.c.k_scale;
   unsigned *per_row = is_v ? (unsigned *)a.c.mass : (unsigned *)a.c.pos;  // of a row, the lanes of its values take the one along, those of its keys the other
   for (int i0 = blockIdx.y * per * kMovesAtOnce + mine; i0 < count; i0 += gridDim.y * per * kMovesAtOnce) {
-    long long to[kMovesAtOnce], of[kMovesAtOnce], to_place[kMovesAtOnce], of_place[kMovesAtOnce];
+    int2 to[kMovesAtOnce], of[kMovesAtOnce];
     u32x4 x[kMovesAtOnce];
     unsigned beside[kMovesAtOnce];
     unsigned char byte[kMovesAtOnce];
-    int to_row[kMovesAtOnce], of_row[kMovesAtOnce];
 #pragma unroll
     for (int m = 0; m < kMovesAtOnce; ++m) {
       const int i = i0 + m * per < count ? i0 + m * per : i0;
-      to_row[m] = place_list[i];
-      of_row[m] = mover_list[i];
+      to[m] = place_list[i];
+      of[m] = mover_list[i];
     }
 #pragma unroll
     for (int m = 0; m < kMovesAtOnce; ++m) {
-      int in_page;
-      int page = page_of(a.c, table, to_row[m], in_page);
-      to[m] = page < 0 ? -1 : row_offset(a.c, page, h, in_page);
-      to_place[m] = row_place(a.c, page, h, in_page);
-      page = page_of(a.c, table, of_row[m], in_page);
-      if (page < 0) to[m] = -1;
-      of[m] = page < 0 ? 0 : row_offset(a.c, page, h, in_page);
-      of_place[m] = row_place(a.c, page, h, in_page);
-    }
-#pragma unroll
-    for (int m = 0; m < kMovesAtOnce; ++m) {
-      x[m] = __builtin_nontemporal_load((const u32x4 *)(pool + of[m] + 16 * piece));
+      if (to[m].x < 0 || of[m].x < 0) to[m].x = of[m].x = -1;
+      const int page = of[m].x < 0 ? 0 : of[m].x, in_page = of[m].x < 0 ? 0 : of[m].y;
+      x[m] = __builtin_nontemporal_load((const u32x4 *)(pool + row_offset(a.c, page, h, in_page) + 16 * piece));
       if (piece == 0) {
-        beside[m] = per_row[to[m] < 0 ? 0 : of_place[m]];
-        if (a.c.e4m3) byte[m] = scale[to[m] < 0 ? 0 : of_place[m]];
+        const long long from = row_place(a.c, page, h, in_page);
+        beside[m] = per_row[from];
+        if (a.c.e4m3) byte[m] = scale[from];
       }
     }
 #pragma unroll
     for (int m = 0; m < kMovesAtOnce; ++m) {
-      if (i0 + m * per < count && to[m] >= 0) {
-        __builtin_nontemporal_store(x[m], (u32x4 *)(pool + to[m] + 16 * piece));
+      if (i0 + m * per < count && to[m].x >= 0) {
+        __builtin_nontemporal_store(x[m], (u32x4 *)(pool + row_offset(a.c, to[m].x, h, to[m].y) + 16 * piece));
         if (piece == 0) {
-          per_row[to_place[m]] = beside[m];
-          if (a.c.e4m3) scale[to_place[m]] = byte[m];
+          const long long place = row_place(a.c, to[m].x, h, to[m].y);
+          per_row[place] = beside[m];
+          if (a.c.e4m3) scale[place] = byte[m];
         }
       }
     }

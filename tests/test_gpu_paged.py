@@ -451,7 +451,7 @@ def test_eviction_leaves_heads_without_the_past_alone():
     assert pool.rows.tolist() == [[150, 50, 150, 50], [100, 50, 100, 50]]
 
 
-@pytest.mark.parametrize("n,keep", [(1023, 512), (1025, 1024), (5000, 200), (40001, 20000), (70001, 69990), (40001, 50000)])
+@pytest.mark.parametrize("n,keep", [(1023, 512), (1025, 1024), (5000, 200), (40001, 20000), (70001, 69990), (40001, 50000), (80003, 40000)])
 def test_eviction_of_long_heads(n, keep):
     pool = Pool(batch=1, hkv=2, d=64, page_rows=64, max_pages=-(-n // 64)).fill([[n, n - 13]])
     _evict(pool, keep, keep // 10, 4)
