@@ -310,6 +310,19 @@ def test_decode_of_ragged_lengths_in_a_roomy_table(kind, d, g, batch, accumulate
     _decode(pool, 2 * g, lengths, accumulate=accumulate)
 
 
+@pytest.mark.parametrize("page_rows", [12, 32])
+def test_weights_of_rows_that_lie_at_any_float(page_rows):
+    lengths = [1, 3, 70, 1030]
+    pool = Pool(batch=4, hkv=2, d=64, page_rows=page_rows, max_pages=-(-1100 // page_rows)).fill(lengths)
+    for shift in (1, 2, 3):
+        room = torch.full((pool.mass.numel() + 7,), 5.0, device="cuda")
+        mass = room[shift:shift + pool.mass.numel()].view(pool.mass.shape)
+        mass.copy_(pool.mass)
+        pool.mass = mass
+        _decode(pool, 4, lengths, accumulate=True)
+        assert (room[:shift] == 5.0).all() and (room[shift + mass.numel():] == 5.0).all()
+
+
 def test_counts_of_many_sequences():
     """More (sequence, head) pairs than a workgroup has threads, in and out of place."""
     B = 700
