@@ -203,7 +203,7 @@ typedef struct {
  * j of all at pos[j] (device int64 [B*rows]: packed batches, caches that were evicted from; not both).  The
  * strides are in elements between token rows, 0 for dense, so that q and k can be parts of one projection's
  * output; heads are dense inside a row; rows and pointers on 16 bytes.  fp32 = 0: bf16, 1: float, in and out.
- * Outputs must not overlap inputs otherwise.  inverse = 1 turns by the negative angles (and multiplies by the
+ * Otherwise an output's rows must not overlap an input's or the other output's (EINVAL).  inverse = 1 turns by the negative angles (and multiplies by the
  * magnitude all the same): applied to the gradients of q_out and k_out it gives those of q and k, for bf16
  * and fp32 results of seg_attn_bwd_* alike.  cfg's rope_theta is not used. */
 segattn_status seg_rope_rotate(const segattn_config *cfg, const segattn_rope *rope, const void *q,
@@ -458,7 +458,7 @@ typedef struct {
  * for one token per sequence (total = B, max_seqlen = 1).  They become rows rows[b,h] on of every KV head, and
  * rows_out[b,h] = rows[b,h] + their number (rows_out may be rows).  Token i of a sequence is at position
  * pos0[b] + i (device int64 [B]; NULL: all 0; below 2^31), which pos gets and, with a rope, the key is turned by; q
- * [total,Hq,D] (NULL: none) is then turned into q_out (may be q).  Without a rope keys are taken as they are
+ * [total,Hq,D] (NULL: none) is then turned into q_out (q itself, or apart from q, k and v).  Without a rope keys are taken as they are
  * (and q is not needed).  mass, where there is one, starts at 0.  e4m3: a row is stored with the smallest
  * power of two 2^e >= 2^-119 for which its largest finite magnitude is at most 448 * 2^e, every element rounded
  * once to nearest even; what is not finite becomes NaN.  bf16: turned keys are rounded once.  A row that has

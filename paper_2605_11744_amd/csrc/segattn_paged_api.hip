@@ -159,6 +159,17 @@ bool overlap(const void *a, const void *b, unsigned long long bytes) {
   return x != y && x < y + bytes && y < x + bytes;
 }
 
+// Rows of two strided tensors, `rows` each, that share bytes.  (Of tensors with different strides only the whole ranges
+// are compared, so parts of rows that lie between each other's are taken for shared ones.)
+bool rows_overlap(const void *x, long long x_row, long long x_stride, const void *y, long long y_row, long long y_stride, long long rows) {
+  const uintptr_t from_x = (uintptr_t)x, from_y = (uintptr_t)y;
+  const __int128 end_x = from_x + (__int128)(rows - 1) * x_stride + x_row, end_y = from_y + (__int128)(rows - 1) * y_stride + y_row;
+  if (from_x >= end_y || from_y >= end_x) return false;
+  if (x_stride != y_stride) return true;
+  const long long off = (long long)(from_y - from_x) % x_stride, at = off < 0 ? off + x_stride : off;  // y's rows in x's
+  return at < x_row || at + y_row > x_stride;
+}
+
 }  // namespace
 
 extern "C" {
@@ -186,8 +197,15 @@ segattn_status seg_rope_rotate(const segattn_config *cfg, const segattn_rope *ro
     if (*t.stride == 0) *t.stride = t.dense;
     if (*t.stride < t.dense || *t.stride >= (1ll << 32) || *t.stride * size % 16 || misaligned(t.at, 16)) return SEGATTN_EINVAL;
   }
-  // in place only row by row: another stride would write over rows that are still to be read
-  if ((q && q == q_out && q_stride != q_out_stride) || (k && k == k_out && k_stride != k_out_stride)) return SEGATTN_EINVAL;
+  // in place only row by row: another place or stride would write over rows that are still to be read
+  const long long total = (long long)p.B * rows;
+  for (int out = 1; out < 4; out += 2) {
+    for (int other = 0; other < 4; ++other) {
+      const auto &x = tensors[out], &y = tensors[other];
+      if (out == other || !x.at || !y.at || (other == out - 1 && x.at == y.at && *x.stride == *y.stride)) continue;
+      if (rows_overlap(x.at, x.dense * size, *x.stride * size, y.at, y.dense * size, *y.stride * size, total)) return SEGATTN_EINVAL;
+    }
+  }
   if (misaligned(pos0, 8) || misaligned(pos, 8) || foreign(stream)) return SEGATTN_EINVAL;
   a.q = q;
   a.k = k;
@@ -199,7 +217,7 @@ segattn_status seg_rope_rotate(const segattn_config *cfg, const segattn_rope *ro
   a.k_out_stride = k_out_stride;
   a.pos0 = (const long long *)pos0;
   a.pos = (const long long *)pos;
-  a.total = (long long)p.B * rows;
+  a.total = total;
   a.rows = (int)rows;
   a.Hq = p.Hq;
   a.Hkv = p.Hkv;
@@ -225,6 +243,9 @@ segattn_status seg_kv_paged_append(const segattn_config *cfg, const segattn_page
       misaligned(rows_out, 4) || misaligned(cu_seqlens, 4) || misaligned(pos0, 8))
     return SEGATTN_EINVAL;
   if (overlap(rows, rows_out, 4ull * p.B * p.Hkv) || overlap(q, q_out, 2ull * total * p.Hq * p.D) || foreign(stream)) return SEGATTN_EINVAL;
+  const long long q_bytes = 2ll * total * p.Hq * p.D, k_bytes = 2ll * total * p.Hkv * p.D;
+  if (q_out && (rows_overlap(q_out, q_bytes, q_bytes, k, k_bytes, k_bytes, 1) || rows_overlap(q_out, q_bytes, q_bytes, v, k_bytes, k_bytes, 1)))
+    return SEGATTN_EINVAL;
   a.q = (const unsigned short *)q;
   a.k = (const unsigned short *)k;
   a.v = (const unsigned short *)v;

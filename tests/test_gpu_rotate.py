@@ -71,6 +71,22 @@ def test_parts_of_a_projection_positions_per_row_and_in_place(inverse, interleav
     assert torch.equal(ref.bits(x[:, hq:]), ref.bits(before[:, hq:])) and (wide[:, hkv:] == 7.0).all()
 
 
+def test_outputs_between_the_inputs_rows():
+    """All four tensors are parts of one [tokens, 2 (Hq + Hkv) D] tensor; then outputs that begin where the inputs end."""
+    n, hq, hkv, d, rope = 67, 4, 2, 64, dict(theta=10000.0)
+    x = torch.randn((n, 2 * (hq + hkv), d), generator=torch.Generator().manual_seed(5)).to(torch.bfloat16).cuda()
+    before, st, pos = x.clone(), torch.cuda.current_stream().cuda_stream, list(range(n))
+    w = x.stride(0)
+    q, k, qo, ko = x.split([hq, hkv, hq, hkv], 1)
+    sa.seg_rope_rotate(_cfg(1, hq, hkv, d), sa.make_rope(**rope), q, k, n, qo, ko, q_stride=w, k_stride=w, q_out_stride=w, k_out_stride=w, stream=st)
+    assert torch.equal(ref.bits(x[:, :hq + hkv]), ref.bits(before[:, :hq + hkv]))
+    _check(qo.contiguous(), q.contiguous(), pos, rope, what="q")
+    _check(ko.contiguous(), k.contiguous(), pos, rope, what="k")
+    y = torch.cat([before[:, :hq].reshape(-1), torch.zeros(n * hq * d, dtype=torch.bfloat16, device="cuda")]).view(2, n, hq, d)
+    sa.seg_rope_rotate(_cfg(1, hq, hkv, d), sa.make_rope(**rope), y[0], None, n, y[1], None, stream=st)
+    _check(y[1], before[:, :hq].contiguous(), pos, rope, what="behind it")
+
+
 def test_one_tensor_alone_and_positions_from_zero():
     rope, cfg = sa.make_rope(theta=10000.0), _cfg(2, 4, 2, 64)
     x = torch.randn((10, 4, 64), device="cuda")

@@ -6,6 +6,7 @@ import pytest
 import paper_2605_11744_amd as sa
 
 P = 4096  # stands for a device pointer: no call below gets as far as using it
+K = P + (1 << 20)  # and for another one
 
 
 def _cfg(**kw):
@@ -45,8 +46,8 @@ BAD_ROPES = [
 
 @pytest.mark.parametrize("bad", BAD_ROPES)
 def test_rotations_that_make_no_sense_are_refused(bad):
-    _refused(sa.seg_rope_rotate, _cfg(), _rope(**bad), P, P, 5, P, P)
-    _refused(sa.seg_kv_paged_append, _cfg(), _pages(), _rope(**bad), P, P, P, None, 2, 1, None, P, P, P)
+    _refused(sa.seg_rope_rotate, _cfg(), _rope(**bad), P, K, 5, P, K)
+    _refused(sa.seg_kv_paged_append, _cfg(), _pages(), _rope(**bad), P, K, K, None, 2, 1, None, P, P, P)
 
 
 @pytest.mark.parametrize("bad", [
@@ -55,7 +56,21 @@ def test_rotations_that_make_no_sense_are_refused(bad):
     dict(pos0=P + 4), dict(pos=P + 4), dict(q_stride=2048), dict(k_stride=512),
 ])
 def test_rotate_refuses_pointers_and_strides(bad):
-    a = dict(q=P, k=P, rows=5, q_out=P, k_out=P)
+    a = dict(q=P, k=K, rows=5, q_out=P, k_out=K)
+    a.update(bad)
+    _refused(sa.seg_rope_rotate, _cfg(), _rope(), a.pop("q"), a.pop("k"), a.pop("rows"), a.pop("q_out"), a.pop("k_out"), **a)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q_out=P + 16), dict(q_out=P - 16), dict(q_out=P + 5 * 2 * 2048 - 16), dict(k_out=P), dict(k_out=K + 512), dict(q_out=K - 16, k_out=K + 8192),
+    dict(q_stride=2048, q_out_stride=4096), dict(q_out=P + 2 * 1008, q_stride=2048, q_out_stride=2048),
+    dict(q_out=P - 2 * 1008, q_stride=2048, q_out_stride=2048), dict(k=P, k_out=P + 2 * 1024, q_stride=1280, q_out_stride=1280, k_stride=1280, k_out_stride=1264),
+    dict(q_out=P + (1 << 16), k_out=P + (1 << 16) + 1024, k_out_stride=1024, q_out_stride=1024),
+    dict(rows=1 << 29, q_stride=(1 << 32) - 8, q_out_stride=(1 << 32) - 8, q_out=P + 16, fp32=True),
+])
+def test_rotate_refuses_outputs_that_share_rows_with_something(bad):
+    """Rows of 1024 and 256 channels; two sequences of five rows unless it says otherwise."""
+    a = dict(q=P, k=K, rows=5, q_out=P, k_out=K)
     a.update(bad)
     _refused(sa.seg_rope_rotate, _cfg(), _rope(), a.pop("q"), a.pop("k"), a.pop("rows"), a.pop("q_out"), a.pop("k_out"), **a)
 
@@ -97,11 +112,11 @@ def test_configurations_without_a_paged_form_are_refused(bad):
 
 
 def test_append_refuses_what_it_cannot_place():
-    ok = dict(q=P, k=P, v=P, cu=P, total=9, longest=5, pos0=P, rows=P, q_out=P, rows_out=P, rope=_rope())
+    ok = dict(q=P, k=K, v=K, cu=P, total=9, longest=5, pos0=P, rows=P, q_out=P, rows_out=P, rope=_rope())
     for bad in (dict(k=None), dict(v=None), dict(rows=None), dict(rows_out=None), dict(q_out=None), dict(q=None), dict(cu=None),
                 dict(cu=None, total=2, longest=2), dict(total=4), dict(total=11), dict(longest=0), dict(total=1 << 31, longest=1 << 30),
                 dict(rope=None, q_out=P + 16), dict(q=P + 2), dict(k=P + 8), dict(pos0=P + 4), dict(rows=P + 1), dict(rows_out=P + 4),
-                dict(q_out=P + 256)):
+                dict(q_out=P + 256), dict(k=P), dict(v=P + 2 * 9 * 1024 - 16), dict(q=K, q_out=K, k=K - 2 * 9 * 256 + 16, v=P)):
         a = {**ok, **bad}
         _refused(sa.seg_kv_paged_append, _cfg(), _pages(), a["rope"], a["q"], a["k"], a["v"], a["cu"], a["total"], a["longest"], a["pos0"],
                  a["rows"], a["q_out"], a["rows_out"])
