@@ -492,7 +492,9 @@ segattn_status seg_attn_decode_paged(const segattn_config *cfg, const segattn_pa
  * other row changes place.  rows_out[b,h] = min(rows[b,h], keep_rows) for a PAST head and rows[b,h] for the others
  * (rows_out may be rows); pages that hold no row any more are the caller's again.  keep_recent + keep_first <=
  * keep_rows.  pages->mass and pages->pos are required, and at least one PAST head.  max_rows as above.
- * A row without a page counts as mass 0.  workspace as above. */
+ * Where the table has holes, a row without a page is not there: rows below keep_rows without one take a place each that nothing can
+ * move to, so as many rows fewer stay (of the protected ones, where not even those have a place, the newest positions
+ * first).  workspace as above. */
 size_t seg_kv_paged_evict_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
                                           int64_t max_rows, int64_t keep_rows);
 segattn_status seg_kv_paged_evict(const segattn_config *cfg, const segattn_pages *pages, const int32_t *rows,

@@ -127,7 +127,7 @@ struct PagedEvictArgs {
   int *moves;           // workspace: rows to move of every window
   unsigned *keys;       // workspace: [window][key_rows], or nullptr where they fit the kernel's LDS
   long long key_rows;
-  int2 *lists;          // workspace: [window][2][most_moves]: freed places, then the rows that go there, as (page or -1, row in it)
+  int2 *lists;          // workspace: [window][2][most_moves]: freed places, then the rows that go there, as (page, row in it)
   int B, Hkv, D;
   int max_rows, keep, recent, first, most_moves;
 };

@@ -1,22 +1,23 @@
 // seg_kv_paged_evict: of every PAST head that holds more than `keep` rows the `keep` with the largest keys stay.
 //
-// A row's key is the bits of its accumulated weight (weights are not negative, so their bits order as they do;
-// what is negative or NaN counts as 0), or the largest of all where its position is among the `recent` newest
-// or the `first` first ones.  Equal keys: the lower row stays.  Rows that stay and lie at or behind row `keep`
-// move, in order, into the places below that become free: attention does not depend on the order of rows, a row
-// is moved at most once, and no place that is read is written, so all rows move at once.
+// A row's key is one more than the bits of its accumulated weight (weights are not negative, so their bits order as they
+// do; what is negative or NaN counts as 0), or above all of those where its position is among the `recent` newest, the
+// newest highest, or the `first` first ones.  Key 0 is a row without a page: it is not there, so it neither stays nor is
+// a place, and as many rows stay as have a page below row `keep`.  Equal keys: the lower row stays.  Rows that stay and
+// lie at or behind row `keep` move, in order, into the places below that become free: attention does not depend on the
+// order of rows, a row is moved at most once, and no place that is read is written, so all rows move at once.
 //
-// select: one workgroup per window finds the key of rank `keep` by counting, a byte of the key at a time, then lists
+// select: one workgroup per window finds the key of the last rank that stays by counting, a byte of the key at a time, then lists
 // the free places and the rows that go there.  move: copies them, many workgroups per window.  Bound by the
-// bytes of the moved rows where many move, else by the passes over the keys: 96 windows of up to 32768 rows to 16384, 46 us
-// for the selection and 82 for 0.38 GB of moves (4.6 TB/s); 32 windows of 1100 to 1279 rows to 1024, 9.9 and 3.9.
+// bytes of the moved rows where many move, else by the passes over the keys: 96 windows of up to 32768 rows to 16384, 48 us
+// for the selection and 82 for 0.38 GB of moves (4.6 TB/s); 32 windows of 1100 to 1279 rows to 1024, 10.5 and 4.
 #include "segattn_paged.h"
 
 namespace segattn {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr unsigned kSureKey = 0xffffffffu;
+constexpr unsigned kNewestKey = 0xffffffffu, kFirstKey = 0x80000000u;  // of the newest position, of the first ones
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kHeldRows = 32 * kSelectThreads;  // rows whose keys fit the select kernel's LDS
 constexpr int kCopies = 4;  // of the histogram: neighbouring lanes count in different ones
@@ -25,7 +26,7 @@ constexpr int kAtOnce = 4;  // rows of a lane that are under way together
 // The select kernel walks over a window's keys seven times, so they are formed once (a key costs a look into the
 // table and two loads) and kept: in LDS (kHeld; the positions in registers until the newest is known), or for longer windows in
 // the workspace.  Wave x has a run of consecutive rows, 64 at a time.  The histogram is kept kCopies times: weights share
-// few exponents, protected rows all bits, and lanes that count the same byte in one word wait for each other.  (Of 11 bits at
+// few exponents, protected rows all but their low bits, and lanes that count the same byte in one word wait for each other.  (Of 11 bits at
 // a time, in one copy: 5.5K rows, 901 of them protected, 18.3 us instead of 17.1.)
 //
 // One compute unit works on a window, and a vector instruction more per 64 rows is 0.25 us more for 32768.  kInPage:
@@ -53,10 +54,10 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
   const int run = (n + kSelectThreads - 1) / kSelectThreads * 64;
   const int r0 = wave * run, r1 = r0 + run < n ? r0 + run : n;
 
-  // First the weights' bits, and the newest position; then the rows that stay for their position's sake.  A row without a
-  // page has weight 0 and no position.
+  // First the weights' bits, and the newest position; then the rows that stay for their position's sake.
   constexpr int kNowhere = -0x7fffffff - 1;
-  int newest = kNowhere;
+  int newest = kNowhere, holes = 0;  // holes: the wave's rows below row keep that have no page
+  const int lo_end = a.keep < r1 ? a.keep : r1;
   // Places of rows r + 64 i + lane, i < kAtOnce, or -1: of the first one of 64 (kInPage) or of the row.  kInPage: the
   // table's entries for 64 steps of the wave are asked at once, one a lane.
   long long place[kAtOnce];
@@ -102,7 +103,8 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const bool held = place[i] >= 0 && r + 64 * i + lane < r1;
-      if (r + 64 * i < r0 + run) keys[r + 64 * i + lane] = held && mass[i] > 0.f ? __float_as_uint(mass[i]) : 0u;
+      if (r + 64 * i < r0 + run) keys[r + 64 * i + lane] = (held && mass[i] > 0.f ? __float_as_uint(mass[i]) : 0u) + held;
+      holes += __popcll(__builtin_amdgcn_ballot_w64(place[i] < 0 && r + 64 * i + lane < lo_end));
       if (!held) pos[i] = kNowhere;
       newest = pos[i] > newest ? pos[i] : newest;
     }
@@ -123,18 +125,28 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
     const int x = __shfl_xor(newest, sh);
     newest = x > newest ? x : newest;
   }
-  if (lane == 0) sm_part[wave][0] = newest;
+  if (lane == 0) *(int2 *)sm_part[wave] = int2{newest, holes};
   __syncthreads();
-  newest = sm_part[0][0];
+  int rank = a.keep;  // rows that stay; below, the edge's rank among the rows that agree with it
 #pragma unroll
-  for (int x = 1; x < kSelectWaves; ++x) newest = sm_part[x][0] > newest ? sm_part[x][0] : newest;
+  for (int x = 0; x < kSelectWaves; ++x) {
+    const int2 of = *(const int2 *)sm_part[x];
+    newest = of.x > newest ? of.x : newest;
+    rank -= of.y;
+  }
+  if (rank == 0) {  // no place below row keep is there
+    if (tid == 0) a.moves[w] = 0;
+    return;
+  }
   // positions above newest - recent stay, as a bound that an int holds
   const int above = (long long)newest - a.recent < kNowhere ? kNowhere : newest - a.recent;
+  const unsigned of_newest = kNewestKey - (unsigned)newest;
   const int from = a.first > 0 ? a.first : kNowhere;
   auto sure = [&](int r, const int (&pos)[kAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i)
-      if ((pos[i] > above || pos[i] < from) && pos[i] != kNowhere) keys[r + 64 * i + lane] = kSureKey;
+      if ((pos[i] > above || pos[i] < from) && pos[i] != kNowhere)
+        keys[r + 64 * i + lane] = pos[i] > above ? (unsigned)pos[i] + of_newest : kFirstKey;
   };
   if constexpr (kHeld) {
 #pragma unroll
@@ -154,8 +166,7 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
     }
   }
   // (a wave reads only the keys that it wrote itself: no barrier)
-  // body(row of lane 0, key) for 64 rows at a time, in order.  The rows from n on have the lowest key, and being the last
-  // ones they lose every tie.
+  // body(row of lane 0, key) for 64 rows at a time, in order.  The rows from n on have key 0 too.
   auto over_rows = [&](auto body) __attribute__((always_inline)) {
     int r = r0;
     for (; r + 64 * 4 <= r0 + run; r += 64 * 4) {
@@ -167,10 +178,9 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
     }
     for (; r < r0 + run; r += 64) body(r, keys[r + lane]);
   };
-  // The key of rank keep, a byte at a time from the top: among the rows that agree with it so far, count by the next
+  // The key of the last row that stays, a byte at a time from the top: among the rows that agree with it so far, count by the next
   // byte and walk down to the one in which the rank falls.
   unsigned edge = 0;
-  int rank = a.keep;  // the edge's rank among the rows that agree with it
   for (int shift = 24; shift >= 0; shift -= 8) {
 #pragma unroll
     for (int i = 0; i < 256 * kCopies / kSelectThreads; ++i) sm_hist[i * kSelectThreads + tid] = 0;
@@ -235,7 +245,7 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
     over_hi += __popcll(over & ~lo);
     on_hi += __popcll(on & ~lo);
   });
-  if (lane == 0) *(int4 *)sm_part[wave] = int4{over_lo, on_lo, over_hi, on_hi};
+  if (lane == 0) *(int4 *)sm_part[wave] = int4{over_lo + holes, on_lo, over_hi, on_hi};
   __syncthreads();
   // lane x < kSelectWaves: wave x's counts; seen: rows on the edge before its rows
   const int4 part = *(const int4 *)sm_part[lane % kSelectWaves];
@@ -281,7 +291,9 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
       seen += __popcll(tie);
     }
     const unsigned long long lo = r + 64 <= a.keep ? ~0ull : r >= a.keep ? 0ull : (1ull << (a.keep - r)) - 1;
-    const unsigned long long pm = ~stays & lo, mm = stays & ~lo;
+    unsigned long long pm = ~stays & lo;
+    const unsigned long long mm = stays & ~lo;
+    if (holes) pm &= __builtin_amdgcn_ballot_w64(key != 0);
     if (kInPage && run > 64 * 64) ask(r);
     if (pm) {
       const int i = places + before(pm);
@@ -324,18 +336,16 @@ __global__ __launch_bounds__(256) void paged_move_kernel(const PagedEvictArgs a)
     }
 #pragma unroll
     for (int m = 0; m < kMovesAtOnce; ++m) {
-      if (to[m].x < 0 || of[m].x < 0) to[m].x = of[m].x = -1;
-      const int page = of[m].x < 0 ? 0 : of[m].x, in_page = of[m].x < 0 ? 0 : of[m].y;
-      x[m] = __builtin_nontemporal_load((const u32x4 *)(pool + row_offset(a.c, page, h, in_page) + 16 * piece));
+      x[m] = __builtin_nontemporal_load((const u32x4 *)(pool + row_offset(a.c, of[m].x, h, of[m].y) + 16 * piece));
       if (piece == 0) {
-        const long long from = row_place(a.c, page, h, in_page);
+        const long long from = row_place(a.c, of[m].x, h, of[m].y);
         beside[m] = per_row[from];
         if (a.c.e4m3) byte[m] = scale[from];
       }
     }
 #pragma unroll
     for (int m = 0; m < kMovesAtOnce; ++m) {
-      if (i0 + m * per < count && to[m].x >= 0) {
+      if (i0 + m * per < count) {
         __builtin_nontemporal_store(x[m], (u32x4 *)(pool + row_offset(a.c, to[m].x, h, to[m].y) + 16 * piece));
         if (piece == 0) {
           const long long place = row_place(a.c, to[m].x, h, to[m].y);

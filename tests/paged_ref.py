@@ -181,24 +181,24 @@ def evicted(pool, keep, recent, first, policy, max_rows=None):
             page, hh, r = pool.place(b, h, range(n))
             ok = page >= 0
             pos = [int(s["pos"][page[i], hh, r[i]]) if ok[i] else None for i in range(n)]
-            newest = max(p for p in pos if p is not None)
+            newest = max((p for p in pos if p is not None), default=0)
             def key(i):
-                if pos[i] is None:
-                    return 0.0
-                if pos[i] > newest - recent or (first > 0 and pos[i] < first):
-                    return math.inf
+                if pos[i] > newest - recent:
+                    return 2, pos[i]
+                if first > 0 and pos[i] < first:
+                    return 1, 0.0
                 m = float(s["mass"][page[i], hh, r[i]])
-                return m if m > 0 else 0.0
-            order = sorted(range(n), key=lambda i: (-key(i), i))
-            kept = set(order[:keep])
-            places = [i for i in range(keep) if i not in kept]
-            movers = [i for i in range(keep, n) if i in kept]
+                return 0, m if m > 0 else 0.0
+            there = [i for i in range(n) if ok[i]]
+            order = sorted(sorted(there), key=key, reverse=True)  # (stable: equal keys stay in the order of rows)
+            kept = set(order[:sum(i < keep for i in there)])
+            places = [i for i in there if i < keep and i not in kept]
+            movers = [i for i in there if i >= keep and i in kept]
             assert len(places) == len(movers)
             for to, of in zip(places, movers):
-                if ok[to] and ok[of]:
-                    for x in s:
-                        if x != "rows":
-                            s[x][page[to], hh, r[to]] = s[x][page[of], hh, r[of]]
-                    moved += 1
+                for x in s:
+                    if x != "rows":
+                        s[x][page[to], hh, r[to]] = s[x][page[of], hh, r[of]]
+                moved += 1
             s["rows"][b, h] = keep
     return s, moved
