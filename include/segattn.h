@@ -491,7 +491,8 @@ segattn_status seg_attn_decode_paged(const segattn_config *cfg, const segattn_pa
  * move, in order, into the rows below that became free, also in order, with their scales, mass and position; no
  * other row changes place.  rows_out[b,h] = min(rows[b,h], keep_rows) for a PAST head and rows[b,h] for the others
  * (rows_out may be rows); pages that hold no row any more are the caller's again.  keep_recent + keep_first <=
- * keep_rows.  pages->mass and pages->pos are required, and at least one PAST head.  max_rows as above.
+ * keep_rows.  pages->mass and pages->pos are required, and at least one PAST head.  max_rows as above: rows
+ * behind it are not looked at, and none of a head where max_rows <= keep_rows.
  * Where the table has holes, a row without a page is not there: rows below keep_rows without one take a place each that nothing can
  * move to, so as many rows fewer stay (of the protected ones, where not even those have a place, the newest positions
  * first).  workspace as above. */

@@ -129,7 +129,8 @@ struct PagedEvictArgs {
   long long key_rows;
   int2 *lists;          // workspace: [window][2][most_moves]: freed places, then the rows that go there, as (page, row in it)
   int B, Hkv, D;
-  int max_rows, keep, recent, first, most_moves;
+  int budget;           // rows that a PAST head may hold afterwards
+  int max_rows, keep, recent, first, most_moves;  // keep: the budget, max_rows at most
 };
 
 hipError_t launch_rotate(const RotateArgs &a, bool fp32, hipStream_t st);

@@ -344,7 +344,8 @@ segattn_status seg_kv_paged_evict(const segattn_config *cfg, const segattn_pages
   a.Hkv = p.Hkv;
   a.D = p.D;
   a.max_rows = (int)max_rows;
-  a.keep = (int)(keep_rows < max_rows ? keep_rows : max_rows);
+  a.budget = (int)(keep_rows < kMostRows ? keep_rows : kMostRows);
+  a.keep = a.budget < a.max_rows ? a.budget : a.max_rows;
   a.recent = (int)(keep_recent < kMostRows ? keep_recent : kMostRows);
   a.first = (int)(keep_first < kMostRows ? keep_first : kMostRows);
   a.most_moves = (int)s.most_moves;

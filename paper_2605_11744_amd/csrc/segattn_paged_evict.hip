@@ -41,9 +41,10 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const Page
   __shared__ int sm_pick[3];
   const int n = rows_held(a.rows, w, a.max_rows);
   __syncthreads();  // rows may be rows_out
-  const bool evicts = in_set(a.heads.past, h) && n > a.keep;
+  const bool past = in_set(a.heads.past, h), evicts = past && n > a.keep;
   if (tid == 0) {
-    a.rows_out[w] = evicts ? a.keep : a.rows[w];
+    const int rows = a.rows[w];
+    a.rows_out[w] = past && rows > a.budget ? a.budget : rows;
     if (!evicts) a.moves[w] = 0;
   }
   if (!evicts) return;
