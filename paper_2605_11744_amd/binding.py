@@ -363,9 +363,17 @@ def make_rope(*, theta: float, rotary_dim: int = 0, interleaved: bool = False, s
     return rope
 
 
+def _check_frequencies(cfg: segattn_config, rope: segattn_rope, where: str) -> None:
+    """The library reads a frequency per pair: a list of another length is refused here, where its length is known."""
+    freq = getattr(rope, "_inv_freq_keepalive", None)
+    if freq is not None and len(freq) != (rope.rotary_dim or cfg.head_dim) // 2:
+        raise SegattnError(SEGATTN_EINVAL, where)
+
+
 def seg_rope_rotate(cfg: segattn_config, rope: segattn_rope, q, k, rows: int, q_out, k_out, *, pos0=None, pos=None,
                     inverse: bool = False, fp32: bool = False, q_stride: int = 0, k_stride: int = 0,
                     q_out_stride: int = 0, k_out_stride: int = 0, stream=None) -> None:
+    _check_frequencies(cfg, rope, "seg_rope_rotate")
     _check(lib().seg_rope_rotate(ctypes.byref(cfg), ctypes.byref(rope), _ptr(q), q_stride, _ptr(k), k_stride, rows,
                                  _ptr(pos0), _ptr(pos), int(inverse), int(fp32), _ptr(q_out), q_out_stride, _ptr(k_out),
                                  k_out_stride, _ptr(stream)), "seg_rope_rotate")
@@ -383,6 +391,8 @@ def make_pages(*, k, v, table, max_pages: int, page_rows: int, n_pages: int, per
 
 def seg_kv_paged_append(cfg: segattn_config, pages: segattn_pages, rope: Optional[segattn_rope], q, k, v, cu_seqlens,
                         total: int, max_seqlen: int, pos0, rows, q_out, rows_out, stream=None) -> None:
+    if rope is not None:
+        _check_frequencies(cfg, rope, "seg_kv_paged_append")
     _check(lib().seg_kv_paged_append(ctypes.byref(cfg), ctypes.byref(pages), ctypes.byref(rope) if rope is not None else None,
                                      _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), total, max_seqlen, _ptr(pos0), _ptr(rows),
                                      _ptr(q_out), _ptr(rows_out), _ptr(stream)), "seg_kv_paged_append")
