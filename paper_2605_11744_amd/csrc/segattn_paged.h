@@ -60,6 +60,20 @@ __device__ inline int rows_held(const int *rows, long long w, int most) {
   return n < 0 ? 0 : n < most ? n : most;
 }
 
+// A launch has fewer than 2^32 threads in a dimension (more are taken modulo 2^32, without an error): a longer row of
+// workgroups goes in several.  launch(first, count) starts workgroups first .. first + count - 1.
+template <typename Launch>
+hipError_t launch_in_parts(long long workgroups, int threads, Launch launch) {
+  const long long most = ((1ll << 32) - 1) / threads;
+  for (long long first = 0; first < workgroups; first += most) {
+    const long long count = workgroups - first < most ? workgroups - first : most;
+    launch(first, (unsigned)count);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // ---- rotation ---------------------------------------------------------------------------------
 struct RotaryArgs {
   int pairs;            // rotary_dim / 2; 0: nothing is turned

@@ -14,11 +14,11 @@ constexpr int kRotateRows = 16;
 // 32K tokens of 32 + 8 heads of 128 took 136 us with 16 tokens, 122 with 4, 118 with 2 (109 with rows marked as not worth
 // keeping: 6.2 TB/s).  Units requested before the sines are formed, or several of a thread at once, are no faster (112).
 template <typename T, bool kInterleaved>
-__global__ __launch_bounds__(256) void rotate_kernel(const RotateArgs a, const int tokens_per_wg) {
+__global__ __launch_bounds__(256) void rotate_kernel(const RotateArgs a, const int tokens_per_wg, const long long first_wg) {
   constexpr int P = 16 / sizeof(T);
   __shared__ __attribute__((aligned(16))) float sm_sn[kRotateRows][64], sm_cs[kRotateRows][64];
   const int tid = threadIdx.x;
-  const long long t0 = (long long)blockIdx.x * tokens_per_wg;
+  const long long t0 = (first_wg + blockIdx.x) * tokens_per_wg;
   const int n = a.total - t0 < tokens_per_wg ? (int)(a.total - t0) : tokens_per_wg;
   const int pairs = a.rot.pairs;
   for (int i = tid; i < n * pairs; i += 256) {
@@ -66,11 +66,11 @@ hipError_t launch_rotate(const RotateArgs &a, bool fp32, hipStream_t st) {
   if (per > a.total / 1024) per = a.total / 1024;
   per = per < 1 ? 1 : per > kRotateRows ? kRotateRows : per;
   const long long blocks = (a.total + per - 1) / per;
-  if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
   const auto kern = fp32 ? (a.rot.interleaved ? rotate_kernel<float, true> : rotate_kernel<float, false>)
                          : (a.rot.interleaved ? rotate_kernel<unsigned short, true> : rotate_kernel<unsigned short, false>);
-  hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), 0, st, a, (int)per);
-  return hipGetLastError();
+  return launch_in_parts(blocks, 256, [&](long long first, unsigned count) {
+    hipLaunchKernelGGL(kern, dim3(count), dim3(256), 0, st, a, (int)per, first);
+  });
 }
 
 }  // namespace segattn
