@@ -55,17 +55,18 @@ __device__ inline void count_rows(const PagedAppendArgs &a, int w) {
 // keys and the values.  The D / 16 threads of a row are neighbours in one wave, which finds an e4m3 row's
 // largest magnitude by exchanges between lanes.
 template <int D, bool kE4m3, bool kInterleaved>
-__global__ __launch_bounds__(256) void paged_append_kernel(const PagedAppendArgs a, const int tokens_per_wg, const int token_wgs) {
+__global__ __launch_bounds__(256) void paged_append_kernel(const PagedAppendArgs a, const int tokens_per_wg, const int token_wgs, const int first_wg) {
   constexpr int kUnits = D / 16;
   __shared__ __attribute__((aligned(16))) float sm_sn[kAppendRows][64], sm_cs[kAppendRows][64];
   __shared__ int sm_seq[kAppendRows], sm_index[kAppendRows];
   __shared__ int2 sm_row[kAppendRows * kMaxKvHeads];  // page (or -1) and row in it
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  if ((int)blockIdx.x >= token_wgs) {
-    count_rows(a, ((int)blockIdx.x - token_wgs) * 256 + tid);
+  const int wg = first_wg + (int)blockIdx.x;
+  if (wg >= token_wgs) {
+    count_rows(a, (wg - token_wgs) * 256 + tid);
     return;
   }
-  const int t0 = (int)blockIdx.x * tokens_per_wg;
+  const int t0 = wg * tokens_per_wg;
   const int n = a.total - t0 < tokens_per_wg ? a.total - t0 : tokens_per_wg;
   // sequence of token t: as many sequences end at or before t
   for (int r = wave; r < n; r += 4) {
@@ -192,8 +193,9 @@ hipError_t launch_paged_append(const PagedAppendArgs &args, hipStream_t st) {
                                            : of(std::make_pair(paged_append_kernel<128, false, false>, paged_append_kernel<128, false, true>)))
                                : (a.c.e4m3 ? of(std::make_pair(paged_append_kernel<64, true, false>, paged_append_kernel<64, true, true>))
                                            : of(std::make_pair(paged_append_kernel<64, false, false>, paged_append_kernel<64, false, true>)));
-  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, a, per, wgs);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = launch_in_parts(grid, 256, [&](long long first, unsigned count) {
+    hipLaunchKernelGGL(kern, dim3(count), dim3(256), 0, st, a, per, wgs, (int)first);
+  });
   if (e != hipSuccess || a.count_rows != 0) return e;
   hipLaunchKernelGGL(paged_count_kernel, dim3(count_wgs), dim3(256), 0, st, a);
   return hipGetLastError();

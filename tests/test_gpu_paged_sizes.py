@@ -30,3 +30,24 @@ def test_rotation_of_more_tokens_than_a_launch_has_workgroups_for():
     for (a, z), b in zip(parts, before):
         want, size = ref.turned(b.double().cpu(), range(a, z), dict(theta=10000.0))
         assert ((x[a:z].double().cpu() - want).abs() <= want.abs() * 2.0 ** -8 * (1 + 2.0 ** -7) + size * 2.0 ** -20).all(), a
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_of_more_tokens_than_a_launch_has_workgroups_for(in_place):
+    """2^26 + 1000 tokens of one head, four a workgroup; pages only for the ends of both sequences."""
+    n, R = (1 << 26) + 1000, 1 << 20
+    new = torch.empty((n, 1, 64), dtype=BF16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    table = torch.full((2, 65), -1, dtype=torch.int32, device="cuda")
+    table[0, 63], table[0, 64], table[1, 0] = 2, 0, 1
+    k, v = (torch.zeros((3, 1, R, 64), dtype=BF16, device="cuda") for _ in "kv")
+    pages = sa.make_pages(k=k, v=v, table=table, max_pages=65, page_rows=R, n_pages=3)
+    rows = torch.tensor([[3], [9]], dtype=torch.int32, device="cuda")
+    out = rows if in_place else torch.full_like(rows, -1)
+    longest = n - 7
+    cu = torch.tensor([0, longest, n], dtype=torch.int32, device="cuda")
+    sa.seg_kv_paged_append(_cfg(2, 1, 1), pages, None, None, new, new, cu, n, longest, None, rows, None, out, _stream())
+    assert out.tolist() == [[longest + 3], [16]]
+    for pool in (k, v):
+        assert torch.equal(pool[2, 0], new[63 * R - 3:64 * R - 3, 0])
+        assert torch.equal(pool[0, 0, :longest + 3 - 64 * R], new[64 * R - 3:longest, 0]) and not pool[0, 0, longest + 3 - 64 * R:].any()
+        assert torch.equal(pool[1, 0, 9:16], new[longest:, 0]) and not pool[1, 0, 16:].any() and not pool[1, 0, :9].any()
