@@ -32,8 +32,8 @@ constexpr int kAtOnce = 4;  // rows of a lane that are under way together
 // One compute unit works on a window, and a vector instruction more per 64 rows is 0.25 us more for 32768.  kInPage:
 // page_rows is a multiple of 64, so 64 rows lie in one page and are found with scalar instructions.
 template <bool kHeld, bool kInPage>
-__global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const PagedEvictArgs a) {
-  const int w = blockIdx.x, b = w / a.Hkv, h = w - b * a.Hkv;
+__global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(const PagedEvictArgs a, const int first_window) {
+  const int w = first_window + blockIdx.x, b = w / a.Hkv, h = w - b * a.Hkv;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   extern __shared__ unsigned sm_keys[];
   __shared__ int sm_hist[256 * kCopies];
@@ -363,21 +363,21 @@ bool evict_keys_held(long long max_rows) { return max_rows <= kHeldRows; }
 hipError_t launch_paged_evict(const PagedEvictArgs &a, hipStream_t st) {
   const int windows = a.B * a.Hkv;
   const bool in_page = a.c.page_rows.d % 64 == 0;
-  if (a.keys) {
-    const auto kern = in_page ? paged_select_kernel<false, true> : paged_select_kernel<false, false>;
-    hipLaunchKernelGGL(kern, dim3(windows), dim3(kSelectThreads), 0, st, a);
-  } else {
-    const auto kern = in_page ? paged_select_kernel<true, true> : paged_select_kernel<true, false>;
+  const auto kern = a.keys ? (in_page ? paged_select_kernel<false, true> : paged_select_kernel<false, false>)
+                           : (in_page ? paged_select_kernel<true, true> : paged_select_kernel<true, false>);
+  int lds = 0;
+  if (!a.keys) {
     static std::atomic<bool> allowed[2];
     if (!allowed[in_page].load(std::memory_order_acquire)) {
       const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kHeldRows * 4);
       if (e != hipSuccess) return e;
       allowed[in_page].store(true, std::memory_order_release);
     }
-    const int lds = a.most_moves ? (a.max_rows + kSelectThreads - 1) / kSelectThreads * kSelectThreads * 4 : 0;  // no window can hold more than it may: nothing is selected
-    hipLaunchKernelGGL(kern, dim3(windows), dim3(kSelectThreads), lds, st, a);
+    if (a.most_moves) lds = (a.max_rows + kSelectThreads - 1) / kSelectThreads * kSelectThreads * 4;  // else no window can hold more than it may: nothing is selected
   }
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = launch_in_parts(windows, kSelectThreads, [&](long long first, unsigned count) {
+    hipLaunchKernelGGL(kern, dim3(count), dim3(kSelectThreads), lds, st, a, (int)first);
+  });
   if (e != hipSuccess || a.most_moves == 0) return e;
   int wgs = 16384 / windows;
   const int at_once = kMovesAtOnce * 256 / (a.D * (a.c.e4m3 ? 2 : 4) / 16);  // rows of a workgroup

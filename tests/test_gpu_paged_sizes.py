@@ -51,3 +51,25 @@ def test_append_of_more_tokens_than_a_launch_has_workgroups_for(in_place):
         assert torch.equal(pool[2, 0], new[63 * R - 3:64 * R - 3, 0])
         assert torch.equal(pool[0, 0, :longest + 3 - 64 * R], new[64 * R - 3:longest, 0]) and not pool[0, 0, longest + 3 - 64 * R:].any()
         assert torch.equal(pool[1, 0, 9:16], new[longest:, 0]) and not pool[1, 0, 16:].any() and not pool[1, 0, :9].any()
+
+
+def test_eviction_of_more_windows_than_a_launch_has_workgroups_for():
+    """32800 sequences of 128 heads, pages for the first and the last one."""
+    B, H = 32800, 128
+    k, v = (torch.randn((2, H, 4, 64), generator=torch.Generator().manual_seed(i)).to(BF16).cuda() for i in range(2))
+    table = torch.full((B, 1), -1, dtype=torch.int32, device="cuda")
+    table[0, 0], table[B - 1, 0] = 1, 0
+    mass = torch.tensor([0.5, 2.0, 1.0, 9.0], device="cuda").expand(2, H, 4).contiguous()
+    pos = torch.tensor([10, 11, 12, 13], dtype=torch.int32, device="cuda").expand(2, H, 4).contiguous()
+    pages = sa.make_pages(k=k, v=v, table=table, max_pages=1, page_rows=4, n_pages=2, mass=mass, pos=pos)
+    rows = torch.full((B, H), 3, dtype=torch.int32, device="cuda")
+    want = [x.clone() for x in (k, v, mass, pos)]
+    for x in want:
+        x[:, :, 0] = x[:, :, 2]  # the heaviest two of three rows stay
+    cfg = _cfg(B, H, H)
+    need = sa.seg_kv_paged_evict_workspace_bytes(cfg, pages, 4, 2)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    sa.seg_kv_paged_evict(cfg, pages, rows, 4, 2, 0, 0, rows, ws, need, _stream())
+    assert (rows == 2).all()
+    for x, y in zip((k, v, mass, pos), want):
+        assert torch.equal(x, y)
