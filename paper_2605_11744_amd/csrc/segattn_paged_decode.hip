@@ -535,13 +535,13 @@ constexpr int kMassRows = 1024;  // rows a workgroup adds the weights of
 // Workgroups 0 .. B Hq - 1: merge of one query head's partials.  The others: weights of kMassRows rows of one PAST
 // head's window, from the scores that the first launch left.
 template <int D>
-__global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecodeArgs a, const int mass_chunks) {
+__global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecodeArgs a, const int mass_chunks, const int first_wg) {
   constexpr int SF = D + kWsTailFloats;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const float c = a.scale_log2e;
-  const int heads = a.B * a.Hq;
-  if ((int)blockIdx.x < heads) {
-    const int b = blockIdx.x / a.Hq, head = blockIdx.x - b * a.Hq, w = b * a.Hkv + head / a.g;
+  const int heads = a.B * a.Hq, wg = first_wg + (int)blockIdx.x;
+  if (wg < heads) {
+    const int b = wg / a.Hq, head = wg - b * a.Hq, w = b * a.Hkv + head / a.g;
     // A partial is read by D / 4 lanes, so a wave has kGroups of them at a time, and kJoinBatch of those under way.
     constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
     __shared__ float sm_m[4], sm_l[4];
@@ -613,7 +613,7 @@ __global__ __launch_bounds__(256) void paged_decode_join_kernel(const PagedDecod
     store_out<D>(a, (long long)b * a.Hq + head, d, o, l, ref);
     return;
   }
-  const int i = blockIdx.x - heads, win = i / mass_chunks, chunk = i - win * mass_chunks;
+  const int i = wg - heads, win = i / mass_chunks, chunk = i - win * mass_chunks;
   const int b = win / a.n_past;
   int h = 0;  // the (win % n_past)-th PAST head
   for (int k = win - b * a.n_past; h < a.Hkv; ++h)
@@ -705,8 +705,9 @@ static hipError_t launch_split(PagedDecodeArgs a, hipStream_t st) {
   const int chunks = kMass ? (a.max_rows + kMassRows - 1) / kMassRows : 0;
   const long long joins = (long long)a.B * a.Hq + (long long)a.B * a.n_past * chunks;
   if (joins > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(paged_decode_join_kernel<D>, dim3((unsigned)joins), dim3(256), 0, st, a, chunks);
-  return hipGetLastError();
+  return launch_in_parts(joins, 256, [&](long long first, unsigned count) {
+    hipLaunchKernelGGL(paged_decode_join_kernel<D>, dim3(count), dim3(256), 0, st, a, chunks, (int)first);
+  });
 }
 template <int D, bool kE4m3, bool kInPage>
 static hipError_t launch_split(const PagedDecodeArgs &a, hipStream_t st) {

@@ -73,3 +73,33 @@ def test_eviction_of_more_windows_than_a_launch_has_workgroups_for():
     assert (rows == 2).all()
     for x, y in zip((k, v, mass, pos), want):
         assert torch.equal(x, y)
+
+
+def test_decode_of_more_heads_than_the_joining_launch_has_workgroups_for():
+    """8200 sequences of 2048 query heads that share a page, a row or two each, in a table with room for windows that are cut."""
+    B, H, g, R = 8200, 128, 16, 8224
+    k, v = (torch.randn((1, H, R, 64), generator=torch.Generator(device="cuda").manual_seed(i), device="cuda", dtype=BF16) for i in range(2))
+    table = torch.zeros((B, 1), dtype=torch.int32, device="cuda")
+    pages = sa.make_pages(k=k, v=v, table=table, max_pages=1, page_rows=R, n_pages=1)
+    rows = torch.ones((B, H), dtype=torch.int32, device="cuda")
+    rows[5], rows[6, 7] = 0, 100
+    cfg = _cfg(B, H * g, H)
+    need = sa.seg_attn_decode_paged_workspace_bytes(cfg, pages, R)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    q = torch.ones((B, H * g, 64), dtype=BF16, device="cuda")
+    out, lse = torch.full_like(q, float("nan")), torch.full((B, H * g), float("nan"), device="cuda")
+    sa.seg_attn_decode_paged(cfg, pages, q, rows, R, out, lse, ws, need, stream=_stream())
+    out = out.view(B, H, g, 64)
+    one = v[0, :, 0][:, None].expand(H, g, 64)  # the only row, with the weight of one
+    score = (k[0, :, 0].double().sum(-1) / 8)[:, None].expand(H, g)
+    delta = 64 * 2.0 ** -24 * float(k[0, :, 0].double().abs().sum(-1).max()) / 8 + 2.0 ** -22 * (1 + float(score.abs().max()))
+    some = torch.ones((B, H), dtype=torch.bool, device="cuda")
+    some[5], some[6, 7] = False, False
+    for b in range(0, B, 200):
+        keep = some[b:b + 200]
+        assert torch.equal(out[b:b + 200][keep], one.expand(200, H, g, 64)[keep])
+        assert ((lse.view(B, H, g)[b:b + 200].double() - score)[keep].abs() <= delta).all()
+    assert (out[5] == 0).all() and (lse[5] == -float("inf")).all()
+    w = torch.softmax(k[0, 7, :100].double().sum(-1) / 8, 0)
+    want = w @ v[0, 7, :100].double()
+    assert ((out[6, 7].double() - want).abs() <= want.abs() * 2.0 ** -8 * (1 + 2.0 ** -7) + 2.0 ** -14 * v[0, 7, :100].double().abs().max()).all()
