@@ -434,7 +434,9 @@ segattn_status seg_attn_decode(segattn_ctx *ctx, const void *q, const void *k_ne
  * validation mode, retrieval mode, past_capacity and rope_theta do not apply here (the first two: EINVAL).
  * Pages may be shared between sequences as long as nobody appends to, evicts from or accumulates weights of
  * them: those calls change the page for everyone who names it, in no fixed order.
- * The current device has to be the stream's and the pointers' (EINVAL for another device's stream). */
+ * The current device has to be the stream's and the pointers' (EINVAL for another device's stream).
+ * Limits (EINVAL): B * Hkv < 2^24; rows of at most 2^26 bytes (row_stride), head_stride and page_stride below 2^40 elements, a
+ * pool below 4e18 bytes. */
 enum { SEGATTN_PAGES_BF16 = 0, SEGATTN_PAGES_E4M3 = 1 };
 typedef struct {
   void *k, *v;            /* device, 16-byte aligned: rows of D elements                             */
@@ -475,7 +477,8 @@ segattn_status seg_kv_paged_append(const segattn_config *cfg, const segattn_page
  * and the workspace, and of a head that holds more only the first max_rows are seen.  accumulate = 1: pages->mass
  * of every row of a PAST head grows by the weight that the row has for this token, summed over the query heads
  * of its group (at least one PAST head, max_rows times the heads of a group below 2^29 -
- * 2^12; EINVAL without mass).  At most 128 query heads per KV head.
+ * 2^12; EINVAL without mass).  At most 128 query heads per KV head, B * Hq < 2^30, and B * Hkv times (the 32-row tiles of max_rows,
+ * plus one) below 2^31.
  * workspace: device, >= ..._workspace_bytes() (0: invalid arguments), 256-byte aligned, overwritten: calls that
  * may overlap need one each. */
 size_t seg_attn_decode_paged_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,

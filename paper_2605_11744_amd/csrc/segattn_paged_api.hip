@@ -128,6 +128,7 @@ bool decode_space(const Problem &p, const PagedCache &c, int64_t max_rows, int a
   if (accumulate && (!c.mass || p.n_past == 0)) return false;
   if (accumulate && (max_rows + kPagedTile) * p.g >= (1ll << 29)) return false;  // the scores of a window are addressed by 31 bits
   const unsigned long long windows = (unsigned long long)p.B * p.Hkv;
+  if ((long long)p.B * p.Hq >= (1ll << 30)) return false;  // (the partials of as many heads would be 290 GB)
   if (windows * ((max_rows + kPagedTile - 1) / kPagedTile + 1) >= (1ull << 31)) return false;
   s.pieces = 0;
   s.slots = align_up(windows * 8ull);

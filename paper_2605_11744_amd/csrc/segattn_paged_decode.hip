@@ -703,8 +703,7 @@ static hipError_t launch_split(PagedDecodeArgs a, hipStream_t st) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int chunks = kMass ? (a.max_rows + kMassRows - 1) / kMassRows : 0;
-  const long long joins = (long long)a.B * a.Hq + (long long)a.B * a.n_past * chunks;
-  if (joins > 0x7fffffffLL) return hipErrorInvalidValue;
+  const long long joins = (long long)a.B * a.Hq + (long long)a.B * a.n_past * chunks;  // < 2^30 + 2^26 + 2^24
   return launch_in_parts(joins, 256, [&](long long first, unsigned count) {
     hipLaunchKernelGGL(paged_decode_join_kernel<D>, dim3(count), dim3(256), 0, st, a, chunks, (int)first);
   });
