@@ -5,8 +5,11 @@
 //   S^T[key][head] = K . Q^T            v_mfma_f32_16x16x32_bf16, A = K rows, B = Q^T (registers)
 //   P = exp2((S^T - m) c)               running maximum m and sum l per head (lane = head), in fp32
 //   O^T[d][head] += V^T . P^T           A = V^T via ds_read_b64_tr_b16, B = P from the S^T registers
-// P enters the product as a bf16 and the bf16 of what that leaves (2^-17 of a weight is lost): the products are
-// idle beside the memory, and the output keeps the accuracy of the type it is rounded to.
+// P enters the product as a bf16 and the bf16 of what that leaves: at most 2^-16 of a weight is lost, where a bf16 output
+// is rounded by up to 2^-8.  For fp32 outputs a third bf16 has the rest, so that all 24 bits count (against the formula 2^-17.2 of
+// the output without it, below 2^-20 with it).  The products are idle beside the memory: fp32 outputs take as long
+// without the third (696 us and 696 for 32 sequences of 4K to 64K, 192 and 194 for 24 of 1K to 32K with 8-bit rows and weights), bf16
+// outputs with it 151 us instead of 143 for those without weights, so it is left out there.
 //
 // The work is bound by memory: every seen row is read once per KV head.  The windows of all (sequence, KV
 // head) pairs are cut into slices of whole tiles, found by the kernel itself from the row counts on the
@@ -364,6 +367,11 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x[h2]), score_rsrc, score_at + t * score_tile + 64 * h2, 0, 0);
     };
 
+    auto values = [&](int nb) __attribute__((always_inline)) {  // V^T, channels 16 nb ..
+      const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[nb]));
+      const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[nb] + 16 * kRow));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
     auto products = [&](int t, unsigned valid) __attribute__((always_inline)) {
       f32x4 S[2];
 #pragma unroll
@@ -389,6 +397,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
       const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * c);
       m_run = m_new;
       bf16x8 P, P_rest;
+      float tail[2][4];  // of a weight beyond its two bf16
       float sum = 0.f;
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2)
@@ -397,7 +406,9 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
           const float e = __builtin_amdgcn_exp2f((S[h2][r] - ref) * c);
           sum += e;
           P[4 * h2 + r] = (__bf16)e;
-          P_rest[4 * h2 + r] = (__bf16)(e - (float)P[4 * h2 + r]);
+          const float rest = e - (float)P[4 * h2 + r];
+          P_rest[4 * h2 + r] = (__bf16)rest;
+          tail[h2][r] = rest - (float)P_rest[4 * h2 + r];
         }
       l_run = l_run * alpha + sum;
       if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {  // a new maximum somewhere: rare behind the first tiles
@@ -406,11 +417,16 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
       }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[nb]));
-        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + voff[nb] + 16 * kRow));
-        const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        const bf16x8 va = values(nb);
         O[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, P, O[nb], 0, 0, 0);
         O[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, P_rest, O[nb], 0, 0, 0);
+      }
+      if (a.out_fp32) {
+        bf16x8 P_tail;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) P_tail[i] = (__bf16)tail[i / 4][i % 4];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) O[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values(nb), P_tail, O[nb], 0, 0, 0);
       }
     };
 
