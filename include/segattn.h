@@ -463,7 +463,8 @@ typedef struct {
  * [total,Hq,D] (NULL: none) is then turned into q_out (q itself, or apart from q, k and v).  Without a rope keys are taken as they are
  * (and q is not needed).  mass, where there is one, starts at 0.  e4m3: a row is stored with the smallest
  * power of two 2^e >= 2^-119 for which its largest finite magnitude is at most 448 * 2^e, every element rounded
- * once to nearest even; what is not finite becomes NaN.  bf16: turned keys are rounded once.  A row that has
+ * once to nearest even; what is not finite becomes NaN, and what is rounded to 2^128 (from 1.9375 * 2^127 on), beyond bf16 and fp32
+ * alike, is infinite to seg_attn_decode_paged.  bf16: turned keys are rounded once.  A row that has
  * no place (no page, or behind the table's last row) is dropped, and rows_out stops at the table's last row. */
 segattn_status seg_kv_paged_append(const segattn_config *cfg, const segattn_pages *pages,
                                    const segattn_rope *rope, const void *q, const void *k, const void *v,

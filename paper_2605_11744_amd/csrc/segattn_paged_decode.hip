@@ -324,7 +324,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_split_kernel(const PagedD
           *(u32x4 *)(tile + r * kRow + (chunk_k(r, piece) << 4)) = xk;
           *(u32x4 *)(tile + kTileBytes + r * kRow + (chunk_v(r, piece) << 4)) = xv;
         } else {
-          // a scale is a power of two and e4m3 has four significant bits: the bf16 is exact
+          // a scale is a power of two and e4m3 has four significant bits: the bf16 is exact below 2^128, and infinite from there on
           const float sk = __uint_as_float((unsigned)__shfl(n_scale, r) << 23), sv = __uint_as_float((unsigned)__shfl(n_scale, r + 32) << 23);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
