@@ -194,8 +194,8 @@ typedef struct {
   double trained_len;    /* > 0, low, high: BY_ROTATIONS and BY_INDEX only                           */
   double low, high;      /* 0 < low < high                                                           */
   double magnitude;      /* >= 0; 0 means 1                                                          */
-  const double *inv_freq;/* host, [rotary_dim / 2] or NULL: the f_i themselves, instead of theta and
-                            scaling (copied)                                                         */
+  const double *inv_freq;/* host, [rotary_dim / 2] or NULL: the f_i themselves (copied); theta and
+                            scaling are then not looked at                                           */
 } segattn_rope;
 
 /* Turns q [B*rows,Hq,D] and k [B*rows,Hkv,D] (B * rows < 2^31 - 4096) into q_out and k_out (either pair may be NULL; in place where the

@@ -31,7 +31,8 @@ bool build_rotary(const segattn_rope *r, int D, RotaryArgs &out) {
   memset(&out, 0, sizeof(out));
   const int n = r->rotary_dim ? r->rotary_dim : D;
   if (n < 16 || n > D || n % 16) return false;
-  if (!(r->theta > 0.0) || isinf(r->theta) || r->interleaved < 0 || r->interleaved > 1) return false;
+  if (r->interleaved < 0 || r->interleaved > 1) return false;
+  if (!r->inv_freq && (!(r->theta > 0.0) || isinf(r->theta))) return false;
   if (!(r->magnitude >= 0.0) || isinf(r->magnitude)) return false;
   const int kind = r->inv_freq ? SEGATTN_ROPE_PLAIN : r->scaling;
   if (kind < SEGATTN_ROPE_PLAIN || kind > SEGATTN_ROPE_BY_INDEX) return false;
@@ -46,7 +47,7 @@ bool build_rotary(const segattn_rope *r, int D, RotaryArgs &out) {
       to = fmin(n - 1.0, ceil(n * log(r->trained_len / (two_pi * r->low)) / (2.0 * log(r->theta))));
     }
   }
-  const double step = -2.0 * log(r->theta) / n;
+  const double step = r->inv_freq ? 0.0 : -2.0 * log(r->theta) / n;
   out.pairs = n / 2;
   out.interleaved = r->interleaved;
   out.magnitude = r->magnitude > 0.0 ? (float)r->magnitude : 1.f;
