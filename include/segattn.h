@@ -198,13 +198,13 @@ typedef struct {
                             scaling are then not looked at                                           */
 } segattn_rope;
 
-/* Turns q [B*rows,Hq,D] and k [B*rows,Hkv,D] (B * rows < 2^31 - 4096) into q_out and k_out (either pair may be NULL; in place where the
- * pointers are the same).  Row t of sequence b is at position pos0[b] + t (device int64 [B]; NULL: all 0), or row
+/* Turns q [B*rows,Hq,D] and k [B*rows,Hkv,D] (B * rows < 2^31 - 4096) into q_out and k_out (either pair may be NULL).  An output may
+ * be its own input (same pointer and stride: in place); apart from that its rows must not overlap an input's or the other
+ * output's (EINVAL).  Row t of sequence b is at position pos0[b] + t (device int64 [B]; NULL: all 0), or row
  * j of all at pos[j] (device int64 [B*rows]: packed batches, caches that were evicted from; not both).  The
  * strides are in elements between token rows, 0 for dense, so that q and k can be parts of one projection's
  * output; heads are dense inside a row; rows and pointers on 16 bytes.  fp32 = 0: bf16, 1: float, in and out.
- * Otherwise an output's rows must not overlap an input's or the other output's (EINVAL).  inverse = 1 turns by the negative angles (and multiplies by the
- * magnitude all the same): applied to the gradients of q_out and k_out it gives those of q and k, for bf16
+ * inverse = 1 turns by the negative angles (and multiplies by the magnitude all the same): applied to the gradients of q_out and k_out it gives those of q and k, for bf16
  * and fp32 results of seg_attn_bwd_* alike.  cfg's rope_theta is not used. */
 segattn_status seg_rope_rotate(const segattn_config *cfg, const segattn_rope *rope, const void *q,
                                int64_t q_stride, const void *k, int64_t k_stride, int64_t rows,
@@ -474,7 +474,7 @@ segattn_status seg_kv_paged_append(const segattn_config *cfg, const segattn_page
 
 /* One decoding step over a paged cache that already holds the newest token's rows (seg_kv_paged_append):
  * q [B,Hq,D] bf16; out [B,Hq,D] bf16 or fp32 (cfg->out_fp32); lse [B,Hq].  A query head that sees no row has
- * zeros and -infinity.  max_rows (host, <= max_pages * page_rows): the most rows of a head; it sizes the launch
+ * zeros and -infinity; one that sees a row of K or V with infinities or NaN may have NaN where the formula has an infinity.  max_rows (host, <= max_pages * page_rows): the most rows of a head; it sizes the launch
  * and the workspace, and of a head that holds more only the first max_rows are seen.  accumulate = 1: pages->mass
  * of every row of a PAST head grows by the weight that the row has for this token, summed over the query heads
  * of its group (at least one PAST head, max_rows times the heads of a group below 2^29 -

@@ -11,13 +11,14 @@
 // without the third (696 us and 696 for 32 sequences of 4K to 64K, 192 and 194 for 24 of 1K to 32K with 8-bit rows and weights), bf16
 // outputs with it 151 us instead of 143 for those without weights, so it is left out there.
 //
-// The work is bound by memory: every seen row is read once per KV head.  The windows of all (sequence, KV
+// The work is bound by memory: every seen row is read once per 16 query heads of its KV head, so a group of up to 16 reads K and V once
+// and one of 128 eight times.  The windows of all (sequence, KV
 // head) pairs are cut into slices of whole tiles, found by the kernel itself from the row counts on the
 // device, so a captured launch serves a cache that grows.  At the end of every window a workgroup writes one
 // partial (acc[D], m, l) per query head; a second launch merges them and, where the cache keeps the weight
-// of its rows, turns the stored scores into weights and adds them up.  Kernels on one card, 8 KV heads of 128: 32
-// sequences of 4K to 64K 664 us + 5 (6.8 TB/s; the read probe reaches 7.15), the same with 8-bit rows 367 + 5; 24 of 1K to 32K with
-// 8-bit rows 144 + 5, with their weights 173 + 18.
+// of its rows, turns the stored scores into weights and adds them up.  Traced kernels on one card, 8 KV
+// heads of 128: 32 sequences of 4K to 64K 700 us + 5 (as calls, untraced, 673: 6.75 TB/s; the read probe reaches 7.15), the same with
+// 8-bit rows 375 + 5; 24 of 1K to 32K with 8-bit rows 143 + 5, with their weights 174 + 19.
 #include "segattn_paged.h"
 
 namespace segattn {

@@ -10,7 +10,7 @@
 // select: one workgroup per window finds the key of the last rank that stays by counting, a byte of the key at a time, then lists
 // the free places and the rows that go there.  move: copies them, many workgroups per window.  Bound by the
 // bytes of the moved rows where many move, else by the passes over the keys: 96 windows of up to 32768 rows to 16384, 48 us
-// for the selection and 82 for 0.38 GB of moves (4.6 TB/s); 32 windows of 1100 to 1279 rows to 1024, 10.5 and 4.
+// for the selection and 83 for 0.38 GB of moves (4.6 TB/s); 32 windows of 1100 to 1279 rows to 1024, 10.9 and 4.3.
 #include "segattn_paged.h"
 
 namespace segattn {

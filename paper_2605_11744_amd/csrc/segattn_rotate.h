@@ -12,7 +12,8 @@
 namespace segattn {
 
 // Sine and cosine of `turns` whole turns, times magnitude.  The turns are formed and reduced to [-1/2, 1/2] in
-// double precision: at position 10^5 a float product is off by 0.01 rad.
+// double precision: at position 10^5 a float product is off by 0.01 rad.  Sine and cosine themselves are formed in 32 bits, which
+// costs fp32 results 3.8e-8 of their size in the mean against 3.6e-8 with ones rounded from 64.
 __device__ inline float2 turn_of(double position, double turns, int back, float magnitude) {
   const double t = position * turns, half = 2.0 * (t - rint(t));
   const float near = (float)half;
