@@ -204,8 +204,9 @@ typedef struct {
  * j of all at pos[j] (device int64 [B*rows]: packed batches, caches that were evicted from; not both).  The
  * strides are in elements between token rows, 0 for dense, so that q and k can be parts of one projection's
  * output; heads are dense inside a row; rows and pointers on 16 bytes.  fp32 = 0: bf16, 1: float, in and out.
- * inverse = 1 turns by the negative angles (and multiplies by the magnitude all the same): applied to the gradients of q_out and k_out it gives those of q and k, for bf16
- * and fp32 results of seg_attn_bwd_* alike.  cfg's rope_theta is not used. */
+ * inverse = 1 turns by the negative angles (and multiplies by the magnitude all the same): applied to the gradients of
+ * q_out and k_out it gives those of q and k, for bf16 and fp32 results of seg_attn_bwd_* alike.  cfg's rope_theta is not
+ * used. */
 segattn_status seg_rope_rotate(const segattn_config *cfg, const segattn_rope *rope, const void *q,
                                int64_t q_stride, const void *k, int64_t k_stride, int64_t rows,
                                const int64_t *pos0, const int64_t *pos, int32_t inverse, int32_t fp32,
@@ -435,8 +436,8 @@ segattn_status seg_attn_decode(segattn_ctx *ctx, const void *q, const void *k_ne
  * Pages may be shared between sequences as long as nobody appends to, evicts from or accumulates weights of
  * them: those calls change the page for everyone who names it, in no fixed order.
  * The current device has to be the stream's and the pointers' (EINVAL for another device's stream).
- * Limits (EINVAL): B * Hkv < 2^24; rows of at most 2^26 bytes (row_stride), head_stride and page_stride below 2^40 elements, a
- * pool below 4e18 bytes. */
+ * Limits (EINVAL): B * Hkv < 2^24; rows of at most 2^26 bytes (row_stride), head_stride and page_stride below 2^40
+ * elements, a pool below 4e18 bytes. */
 enum { SEGATTN_PAGES_BF16 = 0, SEGATTN_PAGES_E4M3 = 1 };
 typedef struct {
   void *k, *v;            /* device, 16-byte aligned: rows of D elements                             */
@@ -474,8 +475,8 @@ segattn_status seg_kv_paged_append(const segattn_config *cfg, const segattn_page
 
 /* One decoding step over a paged cache that already holds the newest token's rows (seg_kv_paged_append):
  * q [B,Hq,D] bf16; out [B,Hq,D] bf16 or fp32 (cfg->out_fp32); lse [B,Hq].  A query head that sees no row has
- * zeros and -infinity; one that sees a row of K or V with infinities or NaN may have NaN where the formula has an infinity.  max_rows (host, <= max_pages * page_rows): the most rows of a head; it sizes the launch
- * and the workspace, and of a head that holds more only the first max_rows are seen.  accumulate = 1: pages->mass
+ * zeros and -infinity; one that sees a row of K or V with infinities or NaN may have NaN where the formula has an
+ * infinity.  max_rows (host, <= max_pages * page_rows): the most rows of a head; it sizes the launch and the workspace, and of a head that holds more only the first max_rows are seen.  accumulate = 1: pages->mass
  * of every row of a PAST head grows by the weight that the row has for this token, summed over the query heads
  * of its group (at least one PAST head, max_rows times the heads of a group below 2^29 -
  * 2^12; EINVAL without mass).  At most 128 query heads per KV head, B * Hq < 2^30, and B * Hkv times (the 32-row tiles of max_rows,
@@ -497,9 +498,9 @@ segattn_status seg_attn_decode_paged(const segattn_config *cfg, const segattn_pa
  * (rows_out may be rows); pages that hold no row any more are the caller's again.  keep_recent + keep_first <=
  * keep_rows.  pages->mass and pages->pos are required, and at least one PAST head.  max_rows as above: rows
  * behind it are not looked at, and none of a head where max_rows <= keep_rows.
- * Where the table has holes, a row without a page is not there: rows below keep_rows without one take a place each that nothing can
- * move to, so as many rows fewer stay (of the protected ones, where not even those have a place, the newest positions
- * first).  workspace as above. */
+ * Where the table has holes, a row without a page is not there: rows below keep_rows without one take a place each that
+ * nothing can move to, so as many rows fewer stay (of the protected ones, where not even those have a place, the newest
+ * positions first).  workspace as above. */
 size_t seg_kv_paged_evict_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
                                           int64_t max_rows, int64_t keep_rows);
 segattn_status seg_kv_paged_evict(const segattn_config *cfg, const segattn_pages *pages, const int32_t *rows,
