@@ -508,6 +508,102 @@ segattn_status seg_kv_paged_evict(const segattn_config *cfg, const segattn_pages
                                   int64_t keep_first, int32_t *rows_out, void *workspace,
                                   size_t workspace_bytes, void *stream);
 
+/* ---- paged cache: tables kept on the device ------------------------------------------------
+ *
+ * users: device int32 [n_pages], how many table entries name a page; a page is free where that is 0 or less.  The two
+ * calls below keep it for the tables that they change: a program that lets a second table name a page adds 1, and a
+ * program whose tables name pages before its first call sets it.  pages->table is written (its entries behind a
+ * sequence's last row have to be unnamed, say -1, where pages are wanted: a named one is taken to be reserved
+ * already).  Both are in stream order and depend on nothing but their inputs. */
+
+/* Pages for tokens that are going to be appended: m of sequence b, cu_seqlens, total and max_seqlen as for
+ * seg_kv_paged_append (there may be fewer tokens than total: cu_seqlens[B] <= total).  Head h wants the entries of rows rows[b,h] ..
+ * rows[b,h] + m - 1, or (newest_only = 1) of those of them that the newest token sees under the head's policy.
+ * Wanted entries that name no page are counted sequence by sequence (with per_head: head by head in it); a
+ * sequence is granted its pages if it needs none, or if the free pages are enough for it and all sequences before it
+ * together, and if its rows fit its table (a sequence whose rows do not fit counts as needing none).  The entries of granted sequences,
+ * in order, get the free pages in ascending order, users of which become 1.  granted[b] (device int32 [B]): 1 or 0; a sequence
+ * that is not granted changes nothing.  slots: device int64 [total,Hkv] or NULL: where the rows of a token will be in
+ * arrays that hold one value per row of the pool (mass, pos, k_scale; rows of a dense pool): ((page * heads) + h) * page_rows + row in
+ * page, h = 0 and heads = 1 with per_head; -1 where the table names no page and for sequences that were not granted.  Tokens from
+ * cu_seqlens[B] on keep theirs.  workspace: device, >= ..._workspace_bytes() (0: invalid arguments), 256-byte aligned, overwritten. */
+size_t seg_kv_paged_reserve_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages);
+segattn_status seg_kv_paged_reserve(const segattn_config *cfg, const segattn_pages *pages, int32_t *users,
+                                    const int32_t *cu_seqlens, int64_t total, int64_t max_seqlen,
+                                    const int32_t *rows, int32_t newest_only, int32_t *granted, int64_t *slots,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* Pages that no head needs any more, given back: an entry that names a page stays if it holds rows of a head (with
+ * per_head: of its head) from the first one that its newest row sees (0 for a PAST head) up to rows[b,h] - 1; any
+ * other becomes -1 and its page loses a user.  rows[b,h] = 0 ends a sequence.  Entries reserved for rows to come
+ * are given back too: call it before reserving, or with the rows that the reservation was for. */
+segattn_status seg_kv_paged_release(const segattn_config *cfg, const segattn_pages *pages, int32_t *users,
+                                    const int32_t *rows, void *stream);
+
+/* ---- paged cache: attention over chosen blocks ----------------------------------------------
+ *
+ * Long-range heads that read a few blocks of their history instead of all of it, chosen anew for every token: a block is
+ * block_rows consecutive rows of a (sequence, KV head), and what it promises a query is bounded from the upper and
+ * lower bounds of its keys in every channel.  Only PAST heads have blocks; the others keep their windows.  One token or many
+ * per sequence: cu_seqlens, total and max_seqlen as for seg_kv_paged_append (cu_seqlens[B] <= total; what belongs to the
+ * tokens from cu_seqlens[B] on is neither read nor written), and the tokens' rows have been appended: token i of
+ * the m of sequence b is row r = rows[b,h] - m + i of head h, and sees no row behind its own.  max_rows (host, <= max_pages *
+ * page_rows): the most rows of a head; it sizes launches and workspaces, and of a head that holds more only the first
+ * max_rows are seen.  At most 128 query heads per KV head. */
+typedef struct {
+  int32_t block_rows;     /* a multiple of 16 that divides page_rows; 64 is a good size           */
+  int8_t *bounds;         /* device, 16-byte aligned, [n_pages][heads][page_rows / block_rows][2][D]: upper, then lower
+                             bounds of a block's keys; heads = 1 with per_head                      */
+  uint8_t *scale;         /* device [n_pages][heads][page_rows / block_rows]: times 2^(byte - 127)    */
+} segattn_blocks;
+
+/* Bounds of the blocks that are complete (all their rows below rows[b,h]) and hold a row from rows_from[b,h] on (device int32
+ * [B,Hkv]; NULL: 0), for every PAST head: after an append with what rows was before it, after an eviction
+ * with NULL.  With e >= -80 the smallest exponent with |k| <= 127 * 2^e for all keys of the block, the bounds are the channels'
+ * largest key / 2^e rounded up and smallest key / 2^e rounded down, and scale = e + 127.  Elements that are not finite in 32
+ * bits count as 0.  max_new (host): the most rows of rows_from .. rows - 1 of a head; of a head with more only the first ones'
+ * blocks are done (the first ceil(max_new / block_rows)).  Blocks in rows without a page are left out.  B * Hkv times ceil(max_new /
+ * block_rows) below 2^40. */
+segattn_status seg_kv_paged_summarize(const segattn_config *cfg, const segattn_pages *pages,
+                                      const segattn_blocks *blocks, const int32_t *rows_from,
+                                      const int32_t *rows, int64_t max_new, void *stream);
+
+/* The n_chosen blocks (1 .. 4096) of every token and PAST head: chosen, device int32 [total,n_past,n_chosen], PAST heads in ascending
+ * order, block numbers (row / block_rows) in ascending order, -1 behind the last.  Of the blocks 0 .. own (that of the token's
+ * own row) all are taken if they are at most n_chosen; else the first keep_first, the last keep_recent (>= 1, so that no
+ * bounds of a block are read that the token cannot see whole; keep_first + keep_recent <= n_chosen), and of the others those
+ * with the highest scores, among equals the lower ones.  With the queries q [total,Hq,D] (bf16) of the KV head's group rounded to
+ * q8 = q / 2^e, to nearest even, e the smallest exponent with |q| <= 127 * 2^e for all of them (elements that are not finite
+ * count as 0), block j's score is
+ *     2^(scale_j - 127) * max over the group of sum over channels of q8 * (q8 > 0 ? upper_j : lower_j),
+ * formed and compared exactly: an upper bound of the block's largest score but for the rounding of q.  A block without a page has the lowest score.
+ * workspace: device, >= ..._workspace_bytes() (0: invalid arguments), 256-byte aligned, overwritten: calls that may overlap need one each. */
+size_t seg_kv_paged_choose_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
+                                           const segattn_blocks *blocks, int64_t total, int64_t max_rows,
+                                           int32_t n_chosen);
+segattn_status seg_kv_paged_choose(const segattn_config *cfg, const segattn_pages *pages,
+                                   const segattn_blocks *blocks, const void *q, const int32_t *cu_seqlens,
+                                   int64_t total, int64_t max_seqlen, const int32_t *rows, int64_t max_rows,
+                                   int32_t n_chosen, int32_t keep_first, int32_t keep_recent, int32_t *chosen,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/* Attention of the tokens q [total,Hq,D] (bf16): a query head of a PAST KV head sees the rows up to its token's own
+ * in the n_chosen (1 .. 65536) listed blocks (chosen as above or the caller's own, in any order: an entry below 0 or behind the
+ * token's block is no block, one that is listed twice counts twice); of another KV head the rows of the token's
+ * window, max(0, s - T) (TAIL) or s up to its own, s the start of its segment.  out [total,Hq,D] bf16 or fp32 (cfg->out_fp32), lse
+ * [total,Hq]; rows without a page are not seen, and a query head that sees no row has zeros and -infinity; one that
+ * sees a row of K or V with infinities or NaN may have NaN where the formula has an infinity, others are not touched by it.  Of
+ * blocks only block_rows is looked at.  chosen may be NULL where no head has the PAST bit (n_chosen is then not looked at).
+ * workspace as above. */
+size_t seg_attn_paged_chosen_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
+                                             const segattn_blocks *blocks, int64_t total, int64_t max_seqlen,
+                                             int64_t max_rows, int32_t n_chosen);
+segattn_status seg_attn_paged_chosen(const segattn_config *cfg, const segattn_pages *pages,
+                                     const segattn_blocks *blocks, const void *q, const int32_t *cu_seqlens,
+                                     int64_t total, int64_t max_seqlen, const int32_t *rows, int64_t max_rows,
+                                     const int32_t *chosen, int32_t n_chosen, void *out, float *lse,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- misc ------------------------------------------------------------------------------- */
 /* Diagnostic for benchmarks: stream `bytes` of device memory at buf (16-byte aligned) with one of
  * the two access patterns of the library's HBM-bound kernels and nothing else.  mode 0: every

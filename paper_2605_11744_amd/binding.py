@@ -54,6 +54,10 @@ class segattn_pages(ctypes.Structure):
                 ("pos", ctypes.c_void_p), ("table", ctypes.c_void_p)]
 
 
+class segattn_blocks(ctypes.Structure):
+    _fields_ = [("block_rows", ctypes.c_int32), ("bounds", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -69,6 +73,7 @@ def lib() -> ctypes.CDLL:
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         cfgp = ctypes.POINTER(segattn_config)
         ropep, pagesp = ctypes.POINTER(segattn_rope), ctypes.POINTER(segattn_pages)
+        blocksp = ctypes.POINTER(segattn_blocks)
         sig = {
             "segattn_cache_bytes": (sz, [cfgp]),
             "segattn_create": (ctypes.c_int, [cfgp, vp, sz, ctypes.POINTER(vp)]),
@@ -107,6 +112,14 @@ def lib() -> ctypes.CDLL:
             "seg_attn_decode_paged": (ctypes.c_int, [cfgp, pagesp, vp, vp, i64, i32, vp, vp, vp, sz, vp]),
             "seg_kv_paged_evict_workspace_bytes": (sz, [cfgp, pagesp, i64, i64]),
             "seg_kv_paged_evict": (ctypes.c_int, [cfgp, pagesp, vp, i64, i64, i64, i64, vp, vp, sz, vp]),
+            "seg_kv_paged_reserve_workspace_bytes": (sz, [cfgp, pagesp]),
+            "seg_kv_paged_reserve": (ctypes.c_int, [cfgp, pagesp, vp, vp, i64, i64, vp, i32, vp, vp, vp, sz, vp]),
+            "seg_kv_paged_release": (ctypes.c_int, [cfgp, pagesp, vp, vp, vp]),
+            "seg_kv_paged_summarize": (ctypes.c_int, [cfgp, pagesp, blocksp, vp, vp, i64, vp]),
+            "seg_kv_paged_choose_workspace_bytes": (sz, [cfgp, pagesp, blocksp, i64, i64, i32]),
+            "seg_kv_paged_choose": (ctypes.c_int, [cfgp, pagesp, blocksp, vp, vp, i64, i64, vp, i64, i32, i32, i32, vp, vp, sz, vp]),
+            "seg_attn_paged_chosen_workspace_bytes": (sz, [cfgp, pagesp, blocksp, i64, i64, i64, i32]),
+            "seg_attn_paged_chosen": (ctypes.c_int, [cfgp, pagesp, blocksp, vp, vp, i64, i64, vp, i64, vp, i32, vp, vp, vp, sz, vp]),
             "segattn_bandwidth_probe": (ctypes.c_int, [vp, sz, i32, vp, vp]),
             "segattn_clock_probe": (ctypes.c_int, [ctypes.c_uint32, vp, ctypes.POINTER(i32), vp]),
             "segattn_mfma_probe": (ctypes.c_int, [i32, i32, vp, ctypes.POINTER(i64), vp]),
@@ -125,7 +138,10 @@ EXPORTS = ("segattn_cache_bytes", "segattn_create", "segattn_destroy", "segattn_
            "seg_attn_fwd_seq", "seg_attn_fwd_varlen", "segattn_layer_policy", "seg_rope_apply", "seg_attn_bwd_workspace_bytes", "seg_attn_bwd_seq", "seg_attn_bwd_seq_static", "seg_attn_bwd_varlen_workspace_bytes", "seg_attn_bwd_varlen", "seg_kv_commit", "seg_kv_commit_seq", "seg_kv_past_append", "seg_kv_past_select", "seg_kv_retrieve_workspace_bytes", "seg_kv_retrieve", "seg_kv_retrieve_seq_workspace_bytes", "seg_kv_retrieve_seq", "seg_attn_fwd_seq_retrieved_workspace_bytes", "seg_attn_fwd_seq_retrieved", "seg_kv_past_evict", "seg_kv_past_keep_recent",
            "seg_kv_lengths", "seg_kv_set_lengths", "segattn_cache_span", "segattn_resident_bytes",
            "seg_attn_decode", "seg_rope_rotate", "seg_kv_paged_append", "seg_attn_decode_paged_workspace_bytes", "seg_attn_decode_paged",
-           "seg_kv_paged_evict_workspace_bytes", "seg_kv_paged_evict", "segattn_bandwidth_probe", "segattn_clock_probe", "segattn_mfma_probe", "segattn_strerror", "segattn_version")
+           "seg_kv_paged_evict_workspace_bytes", "seg_kv_paged_evict",
+           "seg_kv_paged_reserve_workspace_bytes", "seg_kv_paged_reserve", "seg_kv_paged_release", "seg_kv_paged_summarize",
+           "seg_kv_paged_choose_workspace_bytes", "seg_kv_paged_choose", "seg_attn_paged_chosen_workspace_bytes", "seg_attn_paged_chosen",
+           "segattn_bandwidth_probe", "segattn_clock_probe", "segattn_mfma_probe", "segattn_strerror", "segattn_version")
 
 
 def _ptr(x) -> Optional[int]:
@@ -419,3 +435,59 @@ def seg_kv_paged_evict(cfg: segattn_config, pages: segattn_pages, rows, max_rows
     _check(lib().seg_kv_paged_evict(ctypes.byref(cfg), ctypes.byref(pages), _ptr(rows), max_rows, keep_rows, keep_recent,
                                     keep_first, _ptr(rows_out), _ptr(workspace), workspace_bytes, _ptr(stream)),
            "seg_kv_paged_evict")
+
+
+def seg_kv_paged_reserve_workspace_bytes(cfg: segattn_config, pages: segattn_pages) -> int:
+    return int(lib().seg_kv_paged_reserve_workspace_bytes(ctypes.byref(cfg), ctypes.byref(pages)))
+
+
+def seg_kv_paged_reserve(cfg: segattn_config, pages: segattn_pages, users, cu_seqlens, total: int, max_seqlen: int, rows,
+                         granted, slots, workspace, workspace_bytes: int, newest_only: bool = False, stream=None) -> None:
+    _check(lib().seg_kv_paged_reserve(ctypes.byref(cfg), ctypes.byref(pages), _ptr(users), _ptr(cu_seqlens), total, max_seqlen,
+                                      _ptr(rows), int(newest_only), _ptr(granted), _ptr(slots), _ptr(workspace),
+                                      workspace_bytes, _ptr(stream)), "seg_kv_paged_reserve")
+
+
+def seg_kv_paged_release(cfg: segattn_config, pages: segattn_pages, users, rows, stream=None) -> None:
+    _check(lib().seg_kv_paged_release(ctypes.byref(cfg), ctypes.byref(pages), _ptr(users), _ptr(rows), _ptr(stream)),
+           "seg_kv_paged_release")
+
+
+def make_blocks(*, block_rows: int, bounds=None, scale=None) -> segattn_blocks:
+    blocks = segattn_blocks(block_rows, _ptr(bounds), _ptr(scale))
+    blocks._keepalive = (bounds, scale)
+    return blocks
+
+
+def seg_kv_paged_summarize(cfg: segattn_config, pages: segattn_pages, blocks: segattn_blocks, rows_from, rows, max_new: int,
+                           stream=None) -> None:
+    _check(lib().seg_kv_paged_summarize(ctypes.byref(cfg), ctypes.byref(pages), ctypes.byref(blocks), _ptr(rows_from), _ptr(rows),
+                                        max_new, _ptr(stream)), "seg_kv_paged_summarize")
+
+
+def seg_kv_paged_choose_workspace_bytes(cfg: segattn_config, pages: segattn_pages, blocks: segattn_blocks, total: int,
+                                        max_rows: int, n_chosen: int) -> int:
+    return int(lib().seg_kv_paged_choose_workspace_bytes(ctypes.byref(cfg), ctypes.byref(pages), ctypes.byref(blocks), total,
+                                                         max_rows, n_chosen))
+
+
+def seg_kv_paged_choose(cfg: segattn_config, pages: segattn_pages, blocks: segattn_blocks, q, cu_seqlens, total: int,
+                        max_seqlen: int, rows, max_rows: int, n_chosen: int, keep_first: int, keep_recent: int, chosen,
+                        workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib().seg_kv_paged_choose(ctypes.byref(cfg), ctypes.byref(pages), ctypes.byref(blocks), _ptr(q), _ptr(cu_seqlens), total,
+                                     max_seqlen, _ptr(rows), max_rows, n_chosen, keep_first, keep_recent, _ptr(chosen),
+                                     _ptr(workspace), workspace_bytes, _ptr(stream)), "seg_kv_paged_choose")
+
+
+def seg_attn_paged_chosen_workspace_bytes(cfg: segattn_config, pages: segattn_pages, blocks: segattn_blocks, total: int,
+                                          max_seqlen: int, max_rows: int, n_chosen: int) -> int:
+    return int(lib().seg_attn_paged_chosen_workspace_bytes(ctypes.byref(cfg), ctypes.byref(pages), ctypes.byref(blocks), total,
+                                                           max_seqlen, max_rows, n_chosen))
+
+
+def seg_attn_paged_chosen(cfg: segattn_config, pages: segattn_pages, blocks: segattn_blocks, q, cu_seqlens, total: int,
+                          max_seqlen: int, rows, max_rows: int, chosen, n_chosen: int, out, lse, workspace,
+                          workspace_bytes: int, stream=None) -> None:
+    _check(lib().seg_attn_paged_chosen(ctypes.byref(cfg), ctypes.byref(pages), ctypes.byref(blocks), _ptr(q), _ptr(cu_seqlens),
+                                       total, max_seqlen, _ptr(rows), max_rows, _ptr(chosen), n_chosen, _ptr(out), _ptr(lse),
+                                       _ptr(workspace), workspace_bytes, _ptr(stream)), "seg_attn_paged_chosen")

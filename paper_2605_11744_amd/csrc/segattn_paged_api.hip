@@ -2,7 +2,7 @@
 #include <math.h>
 #include <string.h>
 
-#include "segattn_paged.h"
+#include "segattn_sparse.h"
 
 using namespace segattn;
 
@@ -170,6 +170,125 @@ bool rows_overlap(const void *x, long long x_row, long long x_stride, const void
   if (x_stride != y_stride) return true;
   const long long off = (long long)(from_y - from_x) % x_stride, at = off < 0 ? off + x_stride : off;  // y's rows in x's
   return at < x_row || at + y_row > x_stride;
+}
+
+// One of the outputs shares bytes with another one or with an input.
+struct Bytes {
+  const void *at;
+  unsigned long long count;
+};
+template <size_t kOuts, size_t kIns>
+bool shared_bytes(const Bytes (&outs)[kOuts], const Bytes (&ins)[kIns]) {
+  const auto meet = [](const Bytes &x, const Bytes &y) {
+    const unsigned __int128 from_x = (uintptr_t)x.at, from_y = (uintptr_t)y.at;
+    return x.at && y.at && from_x < from_y + y.count && from_y < from_x + x.count;
+  };
+  for (size_t i = 0; i < kOuts; ++i) {
+    for (size_t j = 0; j < i; ++j)
+      if (meet(outs[i], outs[j])) return true;
+    for (size_t j = 0; j < kIns; ++j)
+      if (meet(outs[i], ins[j])) return true;
+  }
+  return false;
+}
+
+unsigned long long table_entries(const Problem &p, const PagedCache &c) {
+  return (unsigned long long)p.B * (c.per_head ? p.Hkv : 1) * c.max_pages;
+}
+
+// A packed batch as the paged operators take it.
+bool batch_fits(const Problem &p, const int32_t *cu_seqlens, int64_t total, int64_t max_seqlen) {
+  if (max_seqlen < 1 || total < max_seqlen || total >= kMostRows || total > (long long)p.B * max_seqlen) return false;
+  return cu_seqlens ? !misaligned(cu_seqlens, 4) : total == p.B && max_seqlen == 1;
+}
+
+struct ReserveSpace {
+  unsigned long long free_of, free, total;
+  long long chunks;
+};
+bool reserve_space(const Problem &p, const PagedCache &c, ReserveSpace &s) {
+  if ((c.per_head ? (long long)p.Hkv : 1ll) * c.max_pages >= kMostRows) return false;
+  s.chunks = ((long long)c.n_pages + kTablePages - 1) / kTablePages;
+  s.free_of = align_up(4ull * p.B);
+  s.free = align_up(s.free_of + 4ull * s.chunks);
+  s.total = s.free + align_up(4ull * c.n_pages);
+  return true;
+}
+
+void fill_tables(const Problem &p, const segattn_pages *pages, PagedTablesArgs &a) {
+  fill_heads(p, a.heads);
+  a.table = const_cast<int32_t *>(pages->table);  // (the caller's device memory; the two calls that write it say so)
+  a.B = p.B;
+  a.Hkv = p.Hkv;
+  a.tail = p.T;
+  a.seg = fast_div_by(p.S);
+}
+
+bool build_blocks(const segattn_blocks *g, const Problem &p, const PagedCache &c, bool bounds, PagedBlocksArgs &a) {
+  if (!g || g->block_rows < 16 || g->block_rows % 16 || (long long)c.page_rows.d % g->block_rows) return false;
+  if (bounds && (!g->bounds || !g->scale || misaligned(g->bounds, 16))) return false;
+  a.c = c;
+  a.bounds = g->bounds;
+  a.scale = g->scale;
+  a.B = p.B;
+  a.Hkv = p.Hkv;
+  a.D = p.D;
+  a.n_past = p.n_past;
+  a.per_page = (int)(c.page_rows.d / g->block_rows);
+  a.block_rows = fast_div_by(g->block_rows);
+  for (int i = 0; i < p.n_past; ++i) a.past[i] = (unsigned char)p.order[i];
+  return true;
+}
+Bytes bounds_bytes(const PagedBlocksArgs &a) { return Bytes{a.bounds, (unsigned long long)a.c.n_pages * a.c.heads * a.per_page * 2 * a.D}; }
+Bytes scale_bytes(const PagedBlocksArgs &a) { return Bytes{a.scale, (unsigned long long)a.c.n_pages * a.c.heads * a.per_page}; }
+
+constexpr long long kMostChosen = 4096, kMostListed = 65536;
+constexpr unsigned long long kChoiceSpace = 256ull << 20;  // keys of as many tokens as fit are formed at a time, of one at least
+bool choose_space(const Problem &p, const PagedBlocksArgs &k, int64_t total, int64_t max_rows, int32_t n_chosen, PagedChooseArgs &a,
+                  unsigned long long &bytes) {
+  if (p.n_past == 0 || p.g > kPagedMostGroup || total < 1 || total >= kMostRows || max_rows < 1 || max_rows > k.c.cap) return false;
+  if (n_chosen < 1 || n_chosen > kMostChosen) return false;
+  a.stride = (max_rows + k.block_rows.d - 1) / k.block_rows.d;
+  const unsigned long long per_token = 4ull * p.n_past * a.stride;
+  unsigned long long part = kChoiceSpace / per_token;
+  part = part < 16 ? 16 : part;
+  a.part = (int)(part < (unsigned long long)total ? part : total);
+  bytes = align_up(a.part * per_token);
+  return true;
+}
+
+bool chosen_space(const Problem &p, const PagedCache &c, const segattn_blocks *blocks, const int32_t *cu_seqlens, int64_t total,
+                  int64_t max_seqlen, int64_t max_rows, int32_t n_chosen, PagedChosenArgs &a, unsigned long long &bytes) {
+  PagedBlocksArgs k;
+  memset(&k, 0, sizeof(k));
+  if (!build_blocks(blocks, p, c, false, k)) return false;
+  if (p.g > kPagedMostGroup || max_rows < 1 || max_rows > c.cap) return false;
+  if (p.n_past && (n_chosen < 1 || n_chosen > kMostListed || (long long)n_chosen * blocks->block_rows >= kMostRows)) return false;
+  a.c = c;
+  a.total = total;
+  a.B = p.B;
+  a.Hq = p.Hq;
+  a.Hkv = p.Hkv;
+  a.g = p.g;
+  a.D = p.D;
+  a.n_past = p.n_past;
+  a.n_other = p.Hkv - p.n_past;
+  a.n_chosen = p.n_past ? n_chosen : 0;
+  a.max_rows = (int)max_rows;
+  a.tail = p.T;
+  a.seg = fast_div_by(p.S);
+  a.block_halves = fast_div_by(blocks->block_rows / 16);
+  a.scale = p.scale;
+  a.scale_log2e = p.scale_log2e;
+  a.out_fp32 = p.out_fp32;
+  a.cu = cu_seqlens;
+  for (int i = 0; i < p.Hkv; ++i) {
+    a.head_of[i] = (unsigned char)p.order[i];
+    a.tail_of[i] = (p.policy[p.order[i]] & SEGATTN_TAIL) != 0;
+  }
+  bytes = align_up(plan_paged_chosen(a, max_seqlen));
+  bytes = bytes ? bytes : kAlign;
+  return true;
 }
 
 }  // namespace
@@ -352,6 +471,172 @@ segattn_status seg_kv_paged_evict(const segattn_config *cfg, const segattn_pages
   a.first = (int)(keep_first < kMostRows ? keep_first : kMostRows);
   a.most_moves = (int)s.most_moves;
   return hip_status(launch_paged_evict(a, (hipStream_t)stream));
+}
+
+size_t seg_kv_paged_reserve_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages) {
+  Problem p;
+  PagedCache c;
+  ReserveSpace s;
+  if (!build_paged(cfg, p) || !build_pages(pages, p, c) || !reserve_space(p, c, s)) return 0;
+  return (size_t)s.total;
+}
+
+segattn_status seg_kv_paged_reserve(const segattn_config *cfg, const segattn_pages *pages, int32_t *users,
+                                    const int32_t *cu_seqlens, int64_t total, int64_t max_seqlen, const int32_t *rows,
+                                    int32_t newest_only, int32_t *granted, int64_t *slots, void *workspace,
+                                    size_t workspace_bytes, void *stream) {
+  Problem p;
+  PagedTablesArgs a;
+  ReserveSpace s;
+  memset(&a, 0, sizeof(a));
+  if (!build_paged(cfg, p) || !build_pages(pages, p, a.c) || !reserve_space(p, a.c, s)) return SEGATTN_EINVAL;
+  if (!users || !rows || !granted || !workspace || workspace_bytes < s.total || newest_only < 0 || newest_only > 1) return SEGATTN_EINVAL;
+  if (!batch_fits(p, cu_seqlens, total, max_seqlen)) return SEGATTN_EINVAL;
+  if (misaligned(users, 4) || misaligned(rows, 4) || misaligned(granted, 4) || misaligned(slots, 8) || misaligned(workspace, kAlign) ||
+      foreign(stream))
+    return SEGATTN_EINVAL;
+  const Bytes outs[] = {{pages->table, 4 * table_entries(p, a.c)}, {users, 4ull * a.c.n_pages}, {granted, 4ull * p.B},
+                        {slots, 8ull * total * p.Hkv}, {workspace, s.total}};
+  const Bytes ins[] = {{rows, 4ull * p.B * p.Hkv}, {cu_seqlens, 4ull * (p.B + 1ull)}};
+  if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+  unsigned char *ws = (unsigned char *)workspace;
+  fill_tables(p, pages, a);
+  a.users = users;
+  a.cu = cu_seqlens;
+  a.rows = rows;
+  a.granted = granted;
+  a.slots = (long long *)slots;
+  a.need = (int *)ws;
+  a.free_of = (int *)(ws + s.free_of);
+  a.free = (int *)(ws + s.free);
+  a.total = total;
+  a.newest = newest_only;
+  a.chunks = (int)s.chunks;
+  return hip_status(launch_paged_reserve(a, (hipStream_t)stream));
+}
+
+segattn_status seg_kv_paged_release(const segattn_config *cfg, const segattn_pages *pages, int32_t *users, const int32_t *rows,
+                                    void *stream) {
+  Problem p;
+  PagedTablesArgs a;
+  memset(&a, 0, sizeof(a));
+  if (!build_paged(cfg, p) || !build_pages(pages, p, a.c)) return SEGATTN_EINVAL;
+  if (!users || !rows || misaligned(users, 4) || misaligned(rows, 4) || foreign(stream)) return SEGATTN_EINVAL;
+  const Bytes outs[] = {{pages->table, 4 * table_entries(p, a.c)}, {users, 4ull * a.c.n_pages}};
+  const Bytes ins[] = {{rows, 4ull * p.B * p.Hkv}};
+  if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+  fill_tables(p, pages, a);
+  a.users = users;
+  a.rows = rows;
+  return hip_status(launch_paged_release(a, (hipStream_t)stream));
+}
+
+segattn_status seg_kv_paged_summarize(const segattn_config *cfg, const segattn_pages *pages, const segattn_blocks *blocks,
+                                      const int32_t *rows_from, const int32_t *rows, int64_t max_new, void *stream) {
+  Problem p;
+  PagedCache c;
+  PagedBlocksArgs a;
+  memset(&a, 0, sizeof(a));
+  if (!build_paged(cfg, p) || !build_pages(pages, p, c) || !build_blocks(blocks, p, c, true, a)) return SEGATTN_EINVAL;
+  if (p.n_past == 0 || !rows || max_new < 1 || max_new >= kMostRows) return SEGATTN_EINVAL;
+  if (misaligned(rows_from, 4) || misaligned(rows, 4) || foreign(stream)) return SEGATTN_EINVAL;
+  const Bytes outs[] = {bounds_bytes(a), scale_bytes(a)};
+  const Bytes ins[] = {{rows, 4ull * p.B * p.Hkv}, {rows_from, 4ull * p.B * p.Hkv}, {pages->table, 4 * table_entries(p, c)}};
+  if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+  a.rows_from = rows_from;
+  a.rows = rows;
+  a.most = (int)((max_new + blocks->block_rows - 1) / blocks->block_rows);
+  a.units = (long long)p.B * p.n_past * a.most;
+  if (a.units >= (1ll << 40)) return SEGATTN_EINVAL;
+  return hip_status(launch_paged_summarize(a, (hipStream_t)stream));
+}
+
+size_t seg_kv_paged_choose_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages, const segattn_blocks *blocks,
+                                           int64_t total, int64_t max_rows, int32_t n_chosen) {
+  Problem p;
+  PagedCache c;
+  PagedChooseArgs a;
+  unsigned long long bytes;
+  memset(&a, 0, sizeof(a));
+  if (!build_paged(cfg, p) || !build_pages(pages, p, c) || !build_blocks(blocks, p, c, true, a.k)) return 0;
+  return choose_space(p, a.k, total, max_rows, n_chosen, a, bytes) ? (size_t)bytes : 0;
+}
+
+segattn_status seg_kv_paged_choose(const segattn_config *cfg, const segattn_pages *pages, const segattn_blocks *blocks, const void *q,
+                                   const int32_t *cu_seqlens, int64_t total, int64_t max_seqlen, const int32_t *rows,
+                                   int64_t max_rows, int32_t n_chosen, int32_t keep_first, int32_t keep_recent, int32_t *chosen,
+                                   void *workspace, size_t workspace_bytes, void *stream) {
+  Problem p;
+  PagedCache c;
+  PagedChooseArgs a;
+  unsigned long long bytes;
+  memset(&a, 0, sizeof(a));
+  if (!build_paged(cfg, p) || !build_pages(pages, p, c) || !build_blocks(blocks, p, c, true, a.k)) return SEGATTN_EINVAL;
+  if (!batch_fits(p, cu_seqlens, total, max_seqlen) || !choose_space(p, a.k, total, max_rows, n_chosen, a, bytes)) return SEGATTN_EINVAL;
+  if (keep_first < 0 || keep_recent < 1 || keep_first > n_chosen - keep_recent || keep_recent > n_chosen) return SEGATTN_EINVAL;
+  if (!q || !rows || !chosen || !workspace || workspace_bytes < bytes) return SEGATTN_EINVAL;
+  if (misaligned(q, 16) || misaligned(rows, 4) || misaligned(chosen, 4) || misaligned(workspace, kAlign) || foreign(stream)) return SEGATTN_EINVAL;
+  const Bytes outs[] = {{chosen, 4ull * total * p.n_past * n_chosen}, {workspace, bytes}};
+  const Bytes ins[] = {{q, 2ull * total * p.Hq * p.D}, {rows, 4ull * p.B * p.Hkv}, {cu_seqlens, 4ull * (p.B + 1ull)},
+                       {pages->table, 4 * table_entries(p, c)}, bounds_bytes(a.k), scale_bytes(a.k)};
+  if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+  a.q = (const unsigned short *)q;
+  a.cu = cu_seqlens;
+  a.k.rows = rows;
+  a.chosen = chosen;
+  a.keys = (unsigned *)workspace;
+  a.total = total;
+  a.Hq = p.Hq;
+  a.g = p.g;
+  a.max_rows = (int)max_rows;
+  a.n_chosen = n_chosen;
+  a.first = keep_first;
+  a.recent = keep_recent;
+  return hip_status(launch_paged_choose(a, (hipStream_t)stream));
+}
+
+size_t seg_attn_paged_chosen_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages, const segattn_blocks *blocks,
+                                             int64_t total, int64_t max_seqlen, int64_t max_rows, int32_t n_chosen) {
+  Problem p;
+  PagedCache c;
+  PagedChosenArgs a;
+  unsigned long long without, with;
+  memset(&a, 0, sizeof(a));
+  if (!build_paged(cfg, p) || !build_pages(pages, p, c)) return 0;
+  if (max_seqlen < 1 || total < max_seqlen || total >= kMostRows || total > (long long)p.B * max_seqlen) return 0;
+  // (the call may come with cu_seqlens or, for one token of every sequence, without)
+  if (!chosen_space(p, c, blocks, nullptr, total, max_seqlen, max_rows, n_chosen, a, without)) return 0;
+  if (!chosen_space(p, c, blocks, (const int32_t *)4, total, max_seqlen, max_rows, n_chosen, a, with)) return 0;
+  return (size_t)(without > with ? without : with);
+}
+
+segattn_status seg_attn_paged_chosen(const segattn_config *cfg, const segattn_pages *pages, const segattn_blocks *blocks, const void *q,
+                                     const int32_t *cu_seqlens, int64_t total, int64_t max_seqlen, const int32_t *rows,
+                                     int64_t max_rows, const int32_t *chosen, int32_t n_chosen, void *out, float *lse,
+                                     void *workspace, size_t workspace_bytes, void *stream) {
+  Problem p;
+  PagedCache c;
+  PagedChosenArgs a;
+  unsigned long long bytes;
+  memset(&a, 0, sizeof(a));
+  if (!build_paged(cfg, p) || !build_pages(pages, p, c) || !batch_fits(p, cu_seqlens, total, max_seqlen)) return SEGATTN_EINVAL;
+  if (!chosen_space(p, c, blocks, cu_seqlens, total, max_seqlen, max_rows, n_chosen, a, bytes)) return SEGATTN_EINVAL;
+  if (!q || !rows || !out || !lse || !workspace || workspace_bytes < bytes || (p.n_past && !chosen)) return SEGATTN_EINVAL;
+  if (misaligned(q, 16) || misaligned(rows, 4) || misaligned(chosen, 4) || misaligned(out, p.out_fp32 ? 4 : 2) || misaligned(lse, 4) ||
+      misaligned(workspace, kAlign) || foreign(stream))
+    return SEGATTN_EINVAL;
+  const unsigned long long heads = (unsigned long long)total * p.Hq;
+  const Bytes outs[] = {{out, heads * p.D * (p.out_fp32 ? 4 : 2)}, {lse, heads * 4}, {workspace, bytes}};
+  const Bytes ins[] = {{q, heads * p.D * 2}, {rows, 4ull * p.B * p.Hkv}, {cu_seqlens, 4ull * (p.B + 1ull)},
+                       {p.n_past ? chosen : nullptr, 4ull * total * p.n_past * n_chosen}, {pages->table, 4 * table_entries(p, c)}};
+  if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+  a.q = (const unsigned short *)q;
+  a.rows = rows;
+  a.chosen = chosen;
+  a.out = out;
+  a.lse = lse;
+  a.slots = (float *)workspace;
+  return hip_status(launch_paged_chosen(a, (hipStream_t)stream));
 }
 
 }  // extern "C"
