@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libsegattn.so")
 SOURCES = ("segattn_api.hip", "segattn_prefill_mfma.hip", "segattn_prefill_keysplit.hip", "segattn_prefill_fp32.hip", "segattn_decode.hip", "segattn_decode_mfma.hip",
            "segattn_cache.hip", "segattn_bwd_fp32.hip", "segattn_bwd_dq.hip", "segattn_bwd_mfma.hip", "segattn_bwd_split.hip", "segattn_rope.hip", "segattn_retrieve.hip", "segattn_probe.hip",
            "segattn_paged_api.hip", "segattn_rotate.hip", "segattn_paged_append.hip", "segattn_paged_decode.hip", "segattn_paged_evict.hip",
-           "segattn_paged_tables.hip", "segattn_paged_blocks.hip", "segattn_paged_chosen.hip")
+           "segattn_paged_tables.hip", "segattn_paged_blocks.hip", "segattn_paged_chosen.hip", "segattn_paged_wide.hip")
 HIPCC_FLAGS = (
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
     # packed fp32 VALU forms are kept out of the generated code on purpose
@@ -29,7 +29,7 @@ HIPCC_FLAGS = (
 _VGPR_FORM = ("-mllvm", "-amdgpu-mfma-vgpr-form=1")
 EXTRA_FLAGS = {"segattn_prefill_mfma.hip": _VGPR_FORM, "segattn_prefill_keysplit.hip": _VGPR_FORM, "segattn_bwd_dq.hip": _VGPR_FORM,
                "segattn_bwd_mfma.hip": _VGPR_FORM, "segattn_bwd_split.hip": _VGPR_FORM, "segattn_paged_decode.hip": _VGPR_FORM,
-               "segattn_paged_chosen.hip": _VGPR_FORM}
+               "segattn_paged_chosen.hip": _VGPR_FORM, "segattn_paged_wide.hip": _VGPR_FORM}
 
 
 def hipcc() -> str:

@@ -258,7 +258,7 @@ bool choose_space(const Problem &p, const PagedBlocksArgs &k, int64_t total, int
 }
 
 bool chosen_space(const Problem &p, const PagedCache &c, const segattn_blocks *blocks, const int32_t *cu_seqlens, int64_t total,
-                  int64_t max_seqlen, int64_t max_rows, int32_t n_chosen, PagedChosenArgs &a, unsigned long long &bytes) {
+                  int64_t max_seqlen, int64_t max_rows, int32_t n_chosen, void *ws, PagedChosenArgs &a, unsigned long long &bytes) {
   PagedBlocksArgs k;
   memset(&k, 0, sizeof(k));
   if (!build_blocks(blocks, p, c, false, k)) return false;
@@ -286,7 +286,7 @@ bool chosen_space(const Problem &p, const PagedCache &c, const segattn_blocks *b
     a.head_of[i] = (unsigned char)p.order[i];
     a.tail_of[i] = (p.policy[p.order[i]] & SEGATTN_TAIL) != 0;
   }
-  bytes = align_up(plan_paged_chosen(a, max_seqlen));
+  bytes = align_up(plan_paged_chosen(a, max_seqlen, (unsigned char *)ws));
   bytes = bytes ? bytes : kAlign;
   return true;
 }
@@ -605,8 +605,8 @@ size_t seg_attn_paged_chosen_workspace_bytes(const segattn_config *cfg, const se
   if (!build_paged(cfg, p) || !build_pages(pages, p, c)) return 0;
   if (max_seqlen < 1 || total < max_seqlen || total >= kMostRows || total > (long long)p.B * max_seqlen) return 0;
   // (the call may come with cu_seqlens or, for one token of every sequence, without)
-  if (!chosen_space(p, c, blocks, nullptr, total, max_seqlen, max_rows, n_chosen, a, without)) return 0;
-  if (!chosen_space(p, c, blocks, (const int32_t *)4, total, max_seqlen, max_rows, n_chosen, a, with)) return 0;
+  if (!chosen_space(p, c, blocks, nullptr, total, max_seqlen, max_rows, n_chosen, nullptr, a, without)) return 0;
+  if (!chosen_space(p, c, blocks, (const int32_t *)4, total, max_seqlen, max_rows, n_chosen, nullptr, a, with)) return 0;
   return (size_t)(without > with ? without : with);
 }
 
@@ -620,7 +620,7 @@ segattn_status seg_attn_paged_chosen(const segattn_config *cfg, const segattn_pa
   unsigned long long bytes;
   memset(&a, 0, sizeof(a));
   if (!build_paged(cfg, p) || !build_pages(pages, p, c) || !batch_fits(p, cu_seqlens, total, max_seqlen)) return SEGATTN_EINVAL;
-  if (!chosen_space(p, c, blocks, cu_seqlens, total, max_seqlen, max_rows, n_chosen, a, bytes)) return SEGATTN_EINVAL;
+  if (!chosen_space(p, c, blocks, cu_seqlens, total, max_seqlen, max_rows, n_chosen, workspace, a, bytes)) return SEGATTN_EINVAL;
   if (!q || !rows || !out || !lse || !workspace || workspace_bytes < bytes || (p.n_past && !chosen)) return SEGATTN_EINVAL;
   if (misaligned(q, 16) || misaligned(rows, 4) || misaligned(chosen, 4) || misaligned(out, p.out_fp32 ? 4 : 2) || misaligned(lse, 4) ||
       misaligned(workspace, kAlign) || foreign(stream))
@@ -635,7 +635,6 @@ segattn_status seg_attn_paged_chosen(const segattn_config *cfg, const segattn_pa
   a.chosen = chosen;
   a.out = out;
   a.lse = lse;
-  a.slots = (float *)workspace;
   return hip_status(launch_paged_chosen(a, (hipStream_t)stream));
 }
 

@@ -65,11 +65,22 @@ struct PagedChosenArgs {
   void *out;
   float *lse;
   float *slots;         // workspace: partials [token][head of the set][part][g], PAST heads before the others
+  // Many tokens at a time: tiles of windows, and listed blocks turned round, a part of the tokens after the other.
+  int wide_windows, by_block;
+  int wide_tokens;      // tokens whose heads are the columns of a window's workgroup
+  int listed_tokens;    // most tokens of a task
+  int listed_pieces;    // of a block, kListedRows rows each
+  int blocks;           // of a window
+  int part_tokens;      // of a part
+  long long part0, entries;       // first token, and entries of the lists
+  int *cursors, *counts;          // workspace: entries and tasks so far; entries of a key (sequence, PAST head, block); together
+  int *offsets, *rank, *sorted;   // where a key's entries lie in `sorted`; an entry's number in its key, -1: sees nothing
+  int4 *tasks;                    // (key, first of its entries in `sorted`, entries)
+  float *listed_out;              // [entry][piece][g][D]
+  float2 *listed_sum;             // [entry][piece][g]: maximum, sum
   long long total;
   int B, Hq, Hkv, g, D, n_past, n_other, n_chosen, max_rows, tail;
   int passes;           // of 16 columns over a token's query heads
-  int tokens;           // of a tile of the other heads
-  long long tiles;      // numbers of such tiles
   int parts_past, parts_other;    // workgroups that share a window
   int tiles_past, tiles_other;    // key tiles of a part
   long long wgs_past, wgs_other;
@@ -80,8 +91,12 @@ struct PagedChosenArgs {
   unsigned char tail_of[kMaxKvHeads];  // the same order: 1 with the TAIL bit
 };
 constexpr int kChosenTile = 32;
-// Shares the windows out (parts, tiles, workgroups); returns the workspace's bytes.
-unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen);
+constexpr int kWideColumns = 128;  // of a window's workgroup
+constexpr int kListedRows = 64;
+// Shares the windows out (parts, tiles, workgroups) and lays the workspace out from `ws` on; returns its bytes.
+unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, unsigned char *ws);
+hipError_t launch_paged_windows(const PagedChosenArgs &a, hipStream_t st);
+hipError_t launch_paged_listed(const PagedChosenArgs &a, hipStream_t st);
 hipError_t launch_paged_chosen(const PagedChosenArgs &a, hipStream_t st);
 
 // The sequence of token t of a packed batch, or -1 (behind the last one); i: its number there, n: the sequence's tokens.

@@ -470,3 +470,41 @@ def test_attention_is_not_touched_by_rows_that_are_not_seen(e4m3):
         pool.v[page.cuda(), hh, i.cuda(), 5] = inf
         out, lse, odd = _attend(pool, 32, [61], 6, hq=8, policy=[2, 1], lists=lists)
         assert odd.any() and out[~odd].isfinite().all()
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=_name)
+def test_attention_of_ragged_tokens_in_bf16(kind):
+    pool, blocks = _pool(kind, [150, 33, [90, 300, 200]], hkv=3)
+    _attend(pool, blocks.rows, [150, 2, 64], 4, hq=12, policy=[1, 2, 3], seg=100, tail=7, out_fp32=False)
+
+
+def test_attention_of_lists_in_parts_of_the_tokens():
+    """More partials than the workspace holds at a time: the tokens go in parts, to the same results as in calls of their own."""
+    pool, _ = _pool(dict(page_rows=256, block=16), [3300], hkv=1)
+    n, chosen, most = 2600, 64, pool.max_pages * pool.R
+    g = torch.Generator().manual_seed(8)
+    q = torch.randn((n, 16, 128), generator=g).to(BF16).cuda()
+    lists = torch.randint(0, 3300 // 16 + 2, (n, 1, chosen), generator=g).to(I32)
+    cfg, blocks = _cfg(pool, 16), sa.make_blocks(block_rows=16)
+    entry = 16 * (128 + 2) * 4  # bytes of an entry's partials
+    assert n * chosen * entry > sa.seg_attn_paged_chosen_workspace_bytes(cfg, pool.pages(), blocks, n, n, most, chosen) > 1000 * chosen * entry
+
+    def call(first, count):
+        out, lse = torch.empty((count, 16, 128), dtype=BF16, device="cuda"), torch.empty((count, 16), device="cuda")
+        rows = torch.tensor([[3300 - (n - first - count)]], dtype=I32, device="cuda")
+        need = sa.seg_attn_paged_chosen_workspace_bytes(cfg, pool.pages(), blocks, count, count, most, chosen)
+        ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+        sa.seg_attn_paged_chosen(cfg, pool.pages(), blocks, q[first:first + count].contiguous(), torch.tensor([0, count], dtype=I32, device="cuda"), count, count,
+                                 rows, most, lists[first:first + count].cuda(), chosen, out, lse, ws, need, stream=_stream())
+        return out, lse
+
+    out, lse = call(0, n)
+    parts = [call(0, 900), call(900, 900), call(1800, 800)]
+    assert torch.equal(out, torch.cat([p[0] for p in parts])) and torch.equal(lse, torch.cat([p[1] for p in parts]))
+    # and the last tokens against the definition
+    last = 5
+    pool.rows[0, 0] = 3300
+    want, want_lse, _, most_s, most_v = sref.attention(pool, q[-last:], [0, last], [[3300]], [2], 64, 16, lists[-last:], 16)
+    delta = 128 * 2.0 ** -24 * most_s + 2.0 ** -20
+    assert ((out[-last:].double().cpu() - want).abs() <= want.abs() * 2.0 ** -8 * (1 + 2.0 ** -7) + (2 * delta + 2.0 ** -16) * most_v).all()
+    assert ((lse[-last:].double().cpu() - want_lse).abs() <= delta + 2.0 ** -22 * (1 + want_lse.abs())).all()
