@@ -592,6 +592,7 @@ segattn_status seg_kv_paged_choose(const segattn_config *cfg, const segattn_page
   a.n_chosen = n_chosen;
   a.first = keep_first;
   a.recent = keep_recent;
+  plan_paged_choose(a, max_seqlen);
   return hip_status(launch_paged_choose(a, (hipStream_t)stream));
 }
 

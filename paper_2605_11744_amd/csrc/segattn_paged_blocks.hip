@@ -137,92 +137,108 @@ __device__ inline unsigned order_key(int dot, int scale) {
 
 // Scores of 16 query rows (tokens of a sequence times a group's heads, padded to a power of two) against 16 blocks at a time:
 //   S[query][block] = [q+ | q-] . [upper | lower]     v_mfma_i32_16x16x64_i8, A = queries, B = bounds, K = 2 D
-// and then the largest over a token's heads.  Units are (tile of tokens, PAST head); a tile's tokens belong to one sequence.
-// GP: heads of a token in a tile, a power of two up to 16; a group of more takes passes of 16.
+// and then the largest over a token's heads.  GP: heads of a token in a tile, a power of two up to 16; a group of more takes passes
+// of 16.
+constexpr int kScoreSets = 4;
 template <int D, int GP>
-__global__ __launch_bounds__(256) void paged_score_kernel(const PagedChooseArgs a, const long long t_first, const long long first_wg, const int wgs_per_unit) {
-  constexpr int NK = D / 64, kTokens = 16 / GP;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, quad = lane >> 4, col = lane & 15;
-  const long long wg = first_wg + blockIdx.x, unit = wg / wgs_per_unit;
-  const int share = (int)(wg - unit * wgs_per_unit);
-  const long long tile = unit / a.k.n_past;
-  const int ph = (int)(unit - tile * a.k.n_past), h = a.k.past[ph];
-  // tokens t0 .. of the part; a tile may meet the ends of sequences: every row of queries has its own
-  const long long t0 = t_first + tile * kTokens;
-  if (t0 >= a.total) return;
-  // sequence of the tile's tokens: tiles go over the tokens end to end, so up to kTokens sequences share one; each is scored
-  // by itself
-  long long t = t0;
-  const long long t_end = t0 + kTokens < a.total ? t0 + kTokens : a.total;
-  while (t < t_end) {
-    int i, n;
-    const int b = sequence_of(a.cu, a.k.B, t, i, n);
-    if (b < 0) return;  // behind the last sequence
-    const int here = (int)(t_end - t < n - i ? t_end - t : n - i);  // tokens of it in the tile
-    const long long w = (long long)b * a.k.Hkv + h;
-    const int seen = rows_seen(a.k.rows, w, i + here - 1, n, a.max_rows);  // of the last one
-    const int own = seen > 0 ? fast_div(seen - 1, a.k.block_rows) : -1;
-    const int hi = own + 1 > a.n_chosen ? own - a.recent + 1 : 0;  // blocks [first, hi) are scored
-    if (hi > a.first) {
-      const int *table = table_of(a.k.c, a.k.Hkv, b, h);
-      // the largest magnitude of every token's queries
-      float most = 0.f;
-      const int passes = (a.g + 15) / 16;
-      const int token = col / GP, head = col % GP;  // of this lane's query row
-      const bool mine = token < here;
-      for (int p = 0; p < passes; ++p) {
-        if (mine && p * 16 + head < a.g) {
-          const unsigned short *q = a.q + ((t + token) * a.Hq + h * a.g + p * 16 + head) * D + 16 * quad;
+struct QueryRows {
+  static constexpr int NK = D / 64;
+  i32x4 up[NK], down[NK];  // this lane's 16 channels of every 64, of row lane % 16: what is above zero, and what is below
+  int shift;               // rounded: q * 2^shift
+
+  __device__ __attribute__((always_inline)) void round(const unsigned short *q) {
 #pragma unroll
-          for (int kc = 0; kc < NK; ++kc)
+    for (int kc = 0; kc < NK; ++kc) {
+      up[kc] = down[kc] = i32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const u32x4 v = *(const u32x4 *)(q + 64 * kc + 8 * half);
+      for (int half = 0; half < 2; ++half) {
+        const u32x4 v = *(const u32x4 *)(q + 64 * kc + 8 * half);
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                most = fmaxf(most, fmaxf(fabsf(finite_or_zero(__uint_as_float(v[e] << 16))), fabsf(finite_or_zero(__uint_as_float(v[e] & 0xffff0000u)))));
-            }
+        for (int e = 0; e < 4; ++e) {
+          const int x0 = (int)rintf(ldexpf(finite_or_zero(__uint_as_float(v[e] << 16)), shift));
+          const int x1 = (int)rintf(ldexpf(finite_or_zero(__uint_as_float(v[e] & 0xffff0000u)), shift));
+          const int word = 2 * half + e / 2, at8 = 16 * (e % 2);
+          up[kc][word] |= ((x0 > 0 ? x0 : 0) << at8) | ((x1 > 0 ? x1 : 0) << (at8 + 8));
+          down[kc][word] |= ((x0 < 0 ? x0 & 255 : 0) << at8) | ((x1 < 0 ? x1 & 255 : 0) << (at8 + 8));
         }
       }
+    }
+  }
+};
+
+// The blocks [first, hi) of the tokens t .. t + here - 1 of sequence b and the PAST head h, by `waves` waves of which this is number
+// `wave`: emit(number of the token, block, key).  QT: sets of 16 query rows that share a block's bounds (1 in passes).
+template <int D, int GP, int QT, typename Emit>
+__device__ __attribute__((always_inline)) void score_blocks(const PagedChooseArgs &a, long long t, int here, int b, int h, int hi, int wave, int waves, Emit emit) {
+  constexpr int NK = D / 64, kAtOnce = QT > 1 ? 1 : 2;  // groups of 16 blocks under way together
+  const int lane = threadIdx.x & 63, quad = lane >> 4, col = lane & 15;
+  const int *table = table_of(a.k.c, a.k.Hkv, b, h);
+  const int passes = GP < 16 ? 1 : (a.g + 15) / 16;
+  QueryRows<D, GP> rows[QT];
+  const unsigned short *q0[QT];
+  const int head = col % GP;  // of this lane's query row
 #pragma unroll
-      for (int sh = 1; sh < GP; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
-      most = fmaxf(most, __shfl_xor(most, 16));
-      most = fmaxf(most, __shfl_xor(most, 32));
-      const int shift = most > 0.f ? -scale_exponent(most) : 0;
-      for (int j0 = a.first + 16 * (wave + 4 * share); j0 < hi; j0 += 64 * wgs_per_unit) {
-        const int j = j0 + col;
-        const BlockAt at = j < hi ? block_at(a.k, table, h, j) : BlockAt{-1, 0};
-        const signed char *bounds = a.k.bounds + (at.block < 0 ? 0 : at.block) * (2 * D) + 16 * quad;
-        i32x4 bd[2 * NK];
+  for (int qt = 0; qt < QT; ++qt) {
+    const int token = qt * (16 / GP) + col / GP;
+    q0[qt] = a.q + ((t + (token < here ? token : 0)) * a.Hq + h * a.g) * D + 16 * quad;
+    // the largest magnitude of every token's queries
+    float most = 0.f;
+    for (int p = 0; p < passes; ++p) {
+      if (p * 16 + head < a.g) {
+        const unsigned short *q = q0[qt] + (p * 16 + head) * D;
 #pragma unroll
-        for (int kc = 0; kc < 2 * NK; ++kc) bd[kc] = *(const i32x4 *)(bounds + 64 * kc);
-        const int scale = a.k.scale[at.block < 0 ? 0 : at.block];
-        int best[4] = {-0x7fffffff - 1, -0x7fffffff - 1, -0x7fffffff - 1, -0x7fffffff - 1};
+        for (int kc = 0; kc < NK; ++kc)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const u32x4 v = *(const u32x4 *)(q + 64 * kc + 8 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              most = fmaxf(most, fmaxf(fabsf(finite_or_zero(__uint_as_float(v[e] << 16))), fabsf(finite_or_zero(__uint_as_float(v[e] & 0xffff0000u)))));
+          }
+      }
+    }
+#pragma unroll
+    for (int sh = 1; sh < GP; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    rows[qt].shift = most > 0.f ? -scale_exponent(most) : 0;
+  }
+  // (rows beyond the group repeat the pass's head 0, which the largest value does not notice)
+  auto take = [&](int qt, int p) __attribute__((always_inline)) { rows[qt].round(q0[qt] + (p * 16 + (p * 16 + head < a.g ? head : 0)) * D); };
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) take(qt, 0);
+  const int step = 16 * kAtOnce * waves;
+  for (int j0 = a.first + 16 * kAtOnce * wave; j0 < hi; j0 += step) {
+    i32x4 bd[kAtOnce][2 * NK];
+    int scale[kAtOnce];
+    bool named[kAtOnce];
+#pragma unroll
+    for (int x = 0; x < kAtOnce; ++x) {
+      const int j = j0 + 16 * x + col;
+      const long long at = j < hi ? block_at(a.k, table, h, j).block : -1;
+      named[x] = at >= 0;
+      const signed char *bounds = a.k.bounds + (named[x] ? at : 0) * (2 * D) + 16 * quad;
+#pragma unroll
+      for (int kc = 0; kc < 2 * NK; ++kc) bd[x][kc] = *(const i32x4 *)(bounds + 64 * kc);
+      scale[x] = a.k.scale[named[x] ? at : 0];
+    }
+#pragma unroll
+    for (int x = 0; x < kAtOnce; ++x) {
+      const int j = j0 + 16 * x + col;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        int best[4];
         for (int p = 0; p < passes; ++p) {
-          const bool live = mine && p * 16 + head < a.g;
-          const unsigned short *q = a.q + ((t + (mine ? token : 0)) * a.Hq + h * a.g + (live ? p * 16 + head : 0)) * D + 16 * quad;
+          if (passes > 1) take(qt, p);
           i32x4 S = {0, 0, 0, 0};
 #pragma unroll
           for (int kc = 0; kc < NK; ++kc) {
-            i32x4 up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const u32x4 v = *(const u32x4 *)(q + 64 * kc + 8 * half);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int x0 = (int)rintf(ldexpf(finite_or_zero(__uint_as_float(v[e] << 16)), shift));
-                const int x1 = (int)rintf(ldexpf(finite_or_zero(__uint_as_float(v[e] & 0xffff0000u)), shift));
-                const int word = 2 * half + e / 2, at8 = 16 * (e % 2);
-                up[word] |= ((x0 > 0 ? x0 : 0) << at8) | ((x1 > 0 ? x1 : 0) << (at8 + 8));
-                down[word] |= ((x0 < 0 ? x0 & 255 : 0) << at8) | ((x1 < 0 ? x1 & 255 : 0) << (at8 + 8));
-              }
-            }
-            S = __builtin_amdgcn_mfma_i32_16x16x64_i8(up, bd[kc], S, 0, 0, 0);
-            S = __builtin_amdgcn_mfma_i32_16x16x64_i8(down, bd[NK + kc], S, 0, 0, 0);
+            S = __builtin_amdgcn_mfma_i32_16x16x64_i8(rows[qt].up[kc], bd[x][kc], S, 0, 0, 0);
+            S = __builtin_amdgcn_mfma_i32_16x16x64_i8(rows[qt].down[kc], bd[x][NK + kc], S, 0, 0, 0);
           }
-          // register r of S: query row 4 quad + r, block col.  The rows beyond the group repeat its head 0 of the pass
+          // register r of S: query row 4 quad + r, block col
 #pragma unroll
-          for (int r = 0; r < 4; ++r) best[r] = S[r] > best[r] ? S[r] : best[r];
+          for (int r = 0; r < 4; ++r) best[r] = p == 0 || S[r] > best[r] ? S[r] : best[r];
         }
         // the largest over the rows of a token
 #pragma unroll
@@ -242,70 +258,142 @@ __global__ __launch_bounds__(256) void paged_score_kernel(const PagedChooseArgs 
         if (j < hi) {
 #pragma unroll
           for (int r = 0; r < 4; r += GP < 4 ? GP : 4) {
-            const int tok = (4 * quad + r) / GP;
-            if (tok < here && (GP <= 4 || (4 * quad) % GP == 0))
-              a.keys[((t + tok - t_first) * a.k.n_past + ph) * a.stride + j] =
-                  at.block < 0 ? 0u : order_key(GP <= 2 ? best[r] : top, scale);
+            const int tok = qt * (16 / GP) + (4 * quad + r) / GP;
+            if (tok < here && (GP <= 4 || (4 * quad) % GP == 0)) emit(tok, j, named[x] ? order_key(GP <= 2 ? best[r] : top, scale[x]) : 0u);
           }
         }
       }
     }
-    t += here;
   }
 }
 
-// A workgroup per (token, PAST head): the n-th largest key digit by digit, then a walk in order.
-__global__ __launch_bounds__(256) void paged_select_kernel(const PagedChooseArgs a, const long long t_first, const long long first_wg) {
-  __shared__ int sm_hist[256], sm_count[4][2];
-  __shared__ unsigned sm_digit;
-  __shared__ int sm_left;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const long long u = first_wg + blockIdx.x, t = t_first + u / a.k.n_past;
-  const int ph = (int)(u % a.k.n_past);
-  int i, n;
-  const int b = sequence_of(a.cu, a.k.B, t, i, n);
-  if (b < 0) return;
-  const int seen = rows_seen(a.k.rows, (long long)b * a.k.Hkv + a.k.past[ph], i, n, a.max_rows);
+// The next tokens of a tile that belong to one sequence: b, and `here` of them from token t on, of which the last sees the blocks up to
+// `hi` - 1 behind the newest ones (0: all of its blocks are taken, nothing is scored).  false: behind the last sequence.
+__device__ inline bool tile_tokens(const PagedChooseArgs &a, long long t, long long t_end, int h, int &b, int &here, int &i, int &n, int &hi) {
+  b = sequence_of(a.cu, a.k.B, t, i, n);
+  if (b < 0) return false;
+  here = (int)(t_end - t < n - i ? t_end - t : n - i);
+  const int seen = rows_seen(a.k.rows, (long long)b * a.k.Hkv + h, i + here - 1, n, a.max_rows);
   const int own = seen > 0 ? fast_div(seen - 1, a.k.block_rows) : -1;
-  int *out = a.chosen + (t * a.k.n_past + ph) * a.n_chosen;
-  if (own + 1 <= a.n_chosen) {
-    for (int x = tid; x < a.n_chosen; x += 256) out[x] = x <= own ? x : -1;
-    return;
+  hi = own + 1 > a.n_chosen ? own - a.recent + 1 : 0;
+  return true;
+}
+
+// Keys to the workspace, where they do not fit LDS.
+template <int D, int GP, int QT>
+__global__ __launch_bounds__(256) void paged_score_kernel(const PagedChooseArgs a, const long long t_first, const long long first_wg, const int wgs_per_unit) {
+  const long long wg = first_wg + blockIdx.x, unit = wg / wgs_per_unit, tile = unit / a.k.n_past;
+  const int share = (int)(wg - unit * wgs_per_unit), ph = (int)(unit - tile * a.k.n_past), h = a.k.past[ph];
+  long long t = t_first + tile * a.tile;
+  const long long t_end = t + a.tile < a.total ? t + a.tile : a.total;
+  int b, here, i, n, hi;
+  for (; t < t_end && tile_tokens(a, t, t_end, h, b, here, i, n, hi); t += here) {
+    if (hi <= a.first) continue;
+    score_blocks<D, GP, QT>(a, t, here, b, h, hi, (threadIdx.x >> 6) + 4 * share, 4 * wgs_per_unit,
+                        [&](int tok, int j, unsigned key) { a.keys[((t + tok - t_first) * a.k.n_past + ph) * a.stride + j] = key; });
   }
-  const int lo = a.first, hi = own - a.recent + 1, picks = a.n_chosen - a.first - a.recent;  // of [lo, hi): more than picks
-  for (int x = tid; x < a.first + a.recent; x += 256) out[x < a.first ? x : picks + x] = x < a.first ? x : hi + x - a.first;
-  if (picks == 0) return;
-  const unsigned *keys = a.keys + u * a.stride;
-  unsigned top = 0;  // digits of the picks-th largest key found so far
-  int left = picks;  // picks among the keys with these digits
-  for (int digit = 3; digit >= 0; --digit) {
-    sm_hist[tid] = 0;
-    __syncthreads();
-    for (int j = lo + tid; j < hi; j += 256) {
-      const unsigned key = keys[j];
-      if (digit == 3 || (key >> (8 * digit + 8)) == top) atomicAdd(&sm_hist[(key >> (8 * digit)) & 255], 1);
+}
+
+// What a list holds besides the picks among [lo, hi): everything where the blocks are few (0 picks left), else the first and the newest ones.
+// By `threads` threads of which this is number `me`.
+__device__ inline int list_frame(const PagedChooseArgs &a, int seen, int *out, int me, int threads, int &hi) {
+  const int own = seen > 0 ? fast_div(seen - 1, a.k.block_rows) : -1;
+  hi = own - a.recent + 1;
+  if (own + 1 <= a.n_chosen) {
+    for (int x = me; x < a.n_chosen; x += threads) out[x] = x <= own ? x : -1;
+    return 0;
+  }
+  const int picks = a.n_chosen - a.first - a.recent;
+  for (int x = me; x < a.first + a.recent; x += threads) out[x < a.first ? x : picks + x] = x < a.first ? x : hi + x - a.first;
+  return picks;
+}
+
+// The `picks` largest of the keys of the blocks [first, hi), more of them than picks, into out[0 ..] in the blocks' order; among equals the
+// lower block.  A lane keeps kHeld keys in registers.  By a team of kWaves waves (1: no barriers) of which this is number `wave`, each with a run of the blocks.  The keys are
+// counted in 256 bins that span them, then those of the bin in which the last pick lies in as many, until a bin's end lies between two
+// picks or the bins are single keys: two or three times.
+template <int kWaves>
+struct Team {
+  int bins[256];
+  unsigned most[kWaves], least[kWaves];
+  int above[kWaves], equal[kWaves];
+  unsigned base;  // of the bin
+  int bin_above, bin_in;
+};
+template <int kWaves, int kHeld = 8, typename Keys>
+__device__ __attribute__((always_inline)) void pick_blocks(const Keys keys, int first, int hi, int picks, int *out, Team<kWaves> &sm, int wave) {
+  const int lane = threadIdx.x & 63, me = wave * 64 + lane;
+  const auto meet = [] {
+    if constexpr (kWaves > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+  };
+  // this wave's run, in whole rounds of 64 blocks
+  const int rounds = (hi - first + 64 * kWaves - 1) / (64 * kWaves);
+  const int from = first + wave * rounds * 64, to = min(hi, from + rounds * 64);
+  unsigned held[kHeld];
+#pragma unroll
+  for (int r = 0; r < kHeld; ++r) held[r] = from + 64 * r + lane < to ? (unsigned)keys[from + 64 * r + lane] : 0u;
+  const auto each = [&](auto what) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r)
+      if (from + 64 * r < to) what(from + 64 * r + lane < to, held[r], from + 64 * r + lane);
+    for (int j = from + 64 * kHeld; j < to; j += 64) what(j + lane < to, j + lane < to ? (unsigned)keys[j + lane] : 0u, j + lane);
+  };
+  unsigned most = 0u, least = ~0u;
+  each([&](bool is, unsigned key, int) {
+    most = is && key > most ? key : most;
+    least = is && key < least ? key : least;
+  });
+#pragma unroll
+  for (int sh = 1; sh < 64; sh <<= 1) {
+    const unsigned y = __shfl_xor(most, sh), z = __shfl_xor(least, sh);
+    most = y > most ? y : most;
+    least = z < least ? z : least;
+  }
+  if constexpr (kWaves > 1) {
+    if (lane == 0) {
+      sm.most[wave] = most;
+      sm.least[wave] = least;
     }
     __syncthreads();
-    if (wave == 0) {  // the digit below which fewer than `left` keys lie above
+    for (int y = 0; y < kWaves; ++y) {
+      most = max(most, sm.most[y]);
+      least = min(least, sm.least[y]);
+    }
+  }
+  // keys from `end` on are picks; those of [base, end) are looked at, `left` of them are picks
+  unsigned base = least, span = most - least;
+  int left = picks;
+  bool exact = false;
+  for (;;) {
+    const int bits = span == 0 ? 0 : 32 - __clz(span), shift = bits > 8 ? bits - 8 : 0;
+    for (int x = me; x < 256; x += 64 * kWaves) sm.bins[x] = 0;
+    meet();
+    each([&](bool is, unsigned key, int) {
+      if (is && key >= base && key - base <= span) atomicAdd(&sm.bins[(key - base) >> shift], 1);
+    });
+    meet();
+    if (wave == 0) {
       int c[4], sum = 0;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        c[x] = sm_hist[255 - (4 * lane + x)];
+        c[x] = sm.bins[255 - (4 * lane + x)];
         sum += c[x];
       }
-      int incl = sum;
+      int before = sum;
 #pragma unroll
       for (int sh = 1; sh < 64; sh <<= 1) {
-        const int up = __shfl_up(incl, sh);
-        if (lane >= sh) incl += up;
+        const int up = __shfl_up(before, sh);
+        if (lane >= sh) before += up;
       }
-      int before = incl - sum;
-      if (before < left && incl >= left) {
+      before -= sum;
+      if (before < left && before + sum >= left) {  // one lane: the bin of the last pick is among its four
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           if (before < left && before + c[x] >= left) {
-            sm_digit = 255 - (4 * lane + x);
-            sm_left = left - before;
+            sm.base = base + ((unsigned)(255 - (4 * lane + x)) << shift);
+            sm.bin_above = before;
+            sm.bin_in = c[x];
             before = 0x40000000;  // found
           } else {
             before += c[x];
@@ -313,68 +401,143 @@ __global__ __launch_bounds__(256) void paged_select_kernel(const PagedChooseArgs
         }
       }
     }
-    __syncthreads();
-    top = (top << 8) | sm_digit;
-    left = sm_left;
-    __syncthreads();
+    meet();
+    base = sm.base;
+    left -= sm.bin_above;
+    exact = sm.bin_in == left;
+    if (exact || shift == 0) break;
+    span = (1u << shift) - 1;
+    meet();  // the bins are read
   }
-  // the blocks above `top`, and the first `left` that equal it
-  int taken = 0, equals = 0;
-  for (int j0 = lo; j0 < hi; j0 += 256) {
-    const int j = j0 + tid;
-    const unsigned key = j < hi ? keys[j] : 0u;
-    const bool equal = j < hi && key == top;
-    const unsigned long long eq = __builtin_amdgcn_ballot_w64(equal), above = __builtin_amdgcn_ballot_w64(j < hi && key > top);
+  // the blocks with keys from `base` on (exact), or above it and of those that equal it the first `left`
+  const auto above = [&](unsigned key) { return exact ? key >= base : key > base; };
+  int place = 0, equals = 0;
+  if constexpr (kWaves > 1) {
+    int n_above = 0, n_equal = 0;
+    each([&](bool is, unsigned key, int) {
+      n_above += __popcll(__builtin_amdgcn_ballot_w64(is && above(key)));
+      n_equal += __popcll(__builtin_amdgcn_ballot_w64(is && !exact && key == base));
+    });
     if (lane == 0) {
-      sm_count[wave][0] = __popcll(above);
-      sm_count[wave][1] = __popcll(eq);
+      sm.above[wave] = n_above;
+      sm.equal[wave] = n_equal;
     }
     __syncthreads();
-    int at = taken, eq_at = equals;
-    for (int x = 0; x < 4; ++x) {
-      if (x < wave) {
-        at += sm_count[x][0];
-        eq_at += sm_count[x][1];
-      }
-      taken += sm_count[x][0];
-      equals += sm_count[x][1];
+    for (int y = 0; y < wave; ++y) {
+      place += sm.above[y];
+      equals += sm.equal[y];
     }
-    const unsigned long long below = (1ull << lane) - 1;
-    at += __popcll(above & below);
-    eq_at += __popcll(eq & below);
-    if ((j < hi && key > top) || (equal && eq_at < left)) out[a.first + at + (eq_at < left ? eq_at : left)] = j;
-    __syncthreads();
   }
-}
-
-template <int D>
-static hipError_t launch_scores(const PagedChooseArgs &a, long long t, long long n, hipStream_t st) {
-  const int gp = a.g <= 1 ? 1 : a.g <= 2 ? 2 : a.g <= 4 ? 4 : a.g <= 8 ? 8 : 16;
-  const long long units = (n + 16 / gp - 1) / (16 / gp) * a.k.n_past;
-  // enough workgroups to fill the card, none with fewer than 64 blocks
-  const long long groups = (a.max_rows / a.k.block_rows.d + 63) / 64;
-  long long share = (2 * device_cus() + units - 1) / units;
-  share = share < 1 ? 1 : share > groups ? (groups < 1 ? 1 : groups) : share;
-  const auto kern = gp == 1 ? paged_score_kernel<D, 1> : gp == 2 ? paged_score_kernel<D, 2> : gp == 4 ? paged_score_kernel<D, 4>
-                    : gp == 8 ? paged_score_kernel<D, 8> : paged_score_kernel<D, 16>;
-  PagedChooseArgs part = a;
-  part.total = t + n;
-  return launch_in_parts(units * share, 256, [&](long long first, unsigned count) {
-    hipLaunchKernelGGL(kern, dim3(count), dim3(256), 0, st, part, t, first, (int)share);
+  if (exact) left = 0;
+  each([&](bool is, unsigned key, int j) {
+    const bool is_above = is && above(key), is_equal = is && !exact && key == base;
+    const unsigned long long ups = __builtin_amdgcn_ballot_w64(is_above), eqs = __builtin_amdgcn_ballot_w64(is_equal), below = (1ull << lane) - 1;
+    const int eq = equals + __popcll(eqs & below);
+    if (is_above || (is_equal && eq < left)) out[place + __popcll(ups & below) + (eq < left ? eq : left)] = j;
+    place += __popcll(ups);
+    equals += __popcll(eqs);
   });
 }
 
-hipError_t launch_paged_choose(const PagedChooseArgs &a, hipStream_t st) {
+// Scores and choice in one launch: a tile's keys stay in LDS.  A token's picks are found by one wave where the tile has several tokens, by
+// all waves together where it has one.
+template <int D, int GP, int kThreads>
+__global__ __launch_bounds__(kThreads) void paged_choose_kernel(const PagedChooseArgs a, const long long first_wg) {
+  constexpr int kWaves = kThreads / 64;
+  extern __shared__ unsigned sm_keys[];  // [token of the tile][stride]
+  __shared__ union {
+    Team<kWaves> all;
+    Team<1> one[kWaves];
+  } sm;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const long long unit = first_wg + blockIdx.x, tile = unit / a.k.n_past;
+  const int ph = (int)(unit - tile * a.k.n_past), h = a.k.past[ph];
+  long long t = tile * a.tile;
+  const long long t_end = t + a.tile < a.total ? t + a.tile : a.total;
+  int b, here, i, n, all_hi;
+  for (; t < t_end && tile_tokens(a, t, t_end, h, b, here, i, n, all_hi); t += here) {
+    if (all_hi > a.first)
+      score_blocks<D, GP, 1>(a, t, here, b, h, all_hi, wave, kWaves, [&](int tok, int j, unsigned key) { sm_keys[tok * a.stride + j] = key; });
+    __syncthreads();
+    const bool together = here == 1;
+    for (int tok = together ? 0 : wave; tok < here; tok += together ? 1 : kWaves) {
+      int *out = a.chosen + ((t + tok) * a.k.n_past + ph) * a.n_chosen;
+      const int seen = rows_seen(a.k.rows, (long long)b * a.k.Hkv + h, i + tok, n, a.max_rows);
+      int hi;
+      const int picks = list_frame(a, seen, out, together ? tid : lane, together ? kThreads : 64, hi);
+      if (picks == 0) continue;
+      if (together) pick_blocks<kWaves>(sm_keys, a.first, hi, picks, out + a.first, sm.all, wave);
+      else pick_blocks<1>(sm_keys + tok * a.stride, a.first, hi, picks, out + a.first, sm.one[wave], 0);
+    }
+    __syncthreads();  // the keys are read
+  }
+}
+
+// The choice from keys in the workspace: a workgroup per (token, PAST head), or (kAlone) a wave.
+template <int kThreads, bool kAlone>
+__global__ __launch_bounds__(kThreads) void paged_select_kernel(const PagedChooseArgs a, const long long t_first, const long long units, const long long first_wg) {
+  constexpr int kTeams = kAlone ? kThreads / 64 : 1, kWaves = kThreads / 64 / kTeams;
+  __shared__ Team<kWaves> sm[kTeams];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), team = kAlone ? wave : 0, me = kAlone ? threadIdx.x & 63 : threadIdx.x;
+  const long long u = (first_wg + blockIdx.x) * kTeams + team, t = t_first + u / a.k.n_past;
+  if (u >= units) return;
+  const int ph = (int)(u % a.k.n_past);
+  int i, n;
+  const int b = sequence_of(a.cu, a.k.B, t, i, n);
+  if (b < 0) return;
+  const int seen = rows_seen(a.k.rows, (long long)b * a.k.Hkv + a.k.past[ph], i, n, a.max_rows);
+  int *out = a.chosen + (t * a.k.n_past + ph) * a.n_chosen;
+  int hi;
+  const int picks = list_frame(a, seen, out, me, 64 * kWaves, hi);
+  if (picks) pick_blocks<kWaves, kAlone ? 16 : 8>(a.keys + u * a.stride, a.first, hi, picks, out + a.first, sm[team], kAlone ? 0 : wave);
+}
+
+template <int D, int GP>
+static hipError_t launch_choose(const PagedChooseArgs &a, hipStream_t st) {
+  if (a.in_lds) {
+    const size_t lds = (size_t)a.tile * a.stride * 4;
+    return launch_in_parts((a.total + a.tile - 1) / a.tile * a.k.n_past, 256, [&](long long first, unsigned count) {
+      hipLaunchKernelGGL((paged_choose_kernel<D, GP, 256>), dim3(count), dim3(256), lds, st, a, first);
+    });
+  }
   for (long long t = 0; t < a.total; t += a.part) {
-    const long long n = a.total - t < a.part ? a.total - t : a.part;
-    hipError_t e = a.k.D == 128 ? launch_scores<128>(a, t, n, st) : launch_scores<64>(a, t, n, st);
+    const long long n = a.total - t < a.part ? a.total - t : a.part, units = n * a.k.n_past, tiles = (n + a.tile - 1) / a.tile * a.k.n_past;
+    // enough workgroups to fill the card, none with fewer than 128 blocks
+    const long long groups = (a.stride + 127) / 128;
+    long long share = (6 * device_cus() + tiles - 1) / tiles;
+    share = share < 1 ? 1 : share > groups ? groups : share;
+    PagedChooseArgs part = a;
+    part.total = t + n;
+    hipError_t e = launch_in_parts(tiles * share, 256, [&](long long first, unsigned count) {
+      if (a.tile > 16 / GP) hipLaunchKernelGGL((paged_score_kernel<D, GP, GP < 16 ? kScoreSets : 1>), dim3(count), dim3(256), 0, st, part, t, first, (int)share);
+      else hipLaunchKernelGGL((paged_score_kernel<D, GP, 1>), dim3(count), dim3(256), 0, st, part, t, first, (int)share);
+    });
     if (e != hipSuccess) return e;
-    e = launch_in_parts(n * a.k.n_past, 256, [&](long long first, unsigned count) {
-      hipLaunchKernelGGL(paged_select_kernel, dim3(count), dim3(256), 0, st, a, t, first);
+    const bool few = units < 2 * device_cus(), many = units >= 16 * device_cus();
+    e = launch_in_parts(many ? (units + 3) / 4 : units, few ? 1024 : 256, [&](long long first, unsigned count) {
+      if (few) hipLaunchKernelGGL((paged_select_kernel<1024, false>), dim3(count), dim3(1024), 0, st, a, t, units, first);
+      else if (many) hipLaunchKernelGGL((paged_select_kernel<256, true>), dim3(count), dim3(256), 0, st, a, t, units, first);
+      else hipLaunchKernelGGL((paged_select_kernel<256, false>), dim3(count), dim3(256), 0, st, a, t, units, first);
     });
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+// Tokens of a tile: one where no sequence has more; as many as 16 query rows hold, or several times as many where the sequences have them.
+void plan_paged_choose(PagedChooseArgs &a, long long max_seqlen) {
+  const int gp = a.g <= 1 ? 1 : a.g <= 2 ? 2 : a.g <= 4 ? 4 : a.g <= 8 ? 8 : 16, set = 16 / gp;
+  a.in_lds = a.stride <= kChoiceInLds;
+  a.tile = max_seqlen == 1 ? 1 : !a.in_lds && gp < 16 && max_seqlen >= 2 * kScoreSets * set ? kScoreSets * set : set;
+}
+
+template <int D>
+static hipError_t launch_choose(const PagedChooseArgs &a, hipStream_t st) {
+  return a.g <= 1 ? launch_choose<D, 1>(a, st) : a.g <= 2 ? launch_choose<D, 2>(a, st) : a.g <= 4 ? launch_choose<D, 4>(a, st)
+         : a.g <= 8 ? launch_choose<D, 8>(a, st) : launch_choose<D, 16>(a, st);
+}
+hipError_t launch_paged_choose(const PagedChooseArgs &a, hipStream_t st) {
+  return a.k.D == 128 ? launch_choose<128>(a, st) : launch_choose<64>(a, st);
 }
 
 }  // namespace segattn

@@ -53,8 +53,12 @@ struct PagedChooseArgs {
   unsigned *keys;       // workspace: [token of the part][n_past][stride]
   long long total, stride;
   int part;             // tokens whose keys the workspace holds
+  int tile;             // tokens of a tile
+  int in_lds;           // a tile's keys fit LDS: no workspace is used
   int Hq, g, max_rows, n_chosen, first, recent;
 };
+constexpr long long kChoiceInLds = 256;  // blocks
+void plan_paged_choose(PagedChooseArgs &a, long long max_seqlen);
 hipError_t launch_paged_choose(const PagedChooseArgs &a, hipStream_t st);
 
 // ---- attention over chosen blocks ---------------------------------------------------------------
