@@ -2,6 +2,8 @@
 //
 // Largest and smallest values do not depend on an order, their scale is a power of two, and a score is a sum of products of
 // 8-bit whole numbers: below 2 * 128 * 2^14 in magnitude, so that it is the same however it is formed, and so is the choice.
+#include <type_traits>
+
 #include "segattn_sparse.h"
 
 namespace segattn {
@@ -31,10 +33,26 @@ __device__ inline BlockAt block_at(const PagedBlocksArgs &a, const int *table, i
   return BlockAt{((long long)page * a.c.heads + hh) * a.per_page + fast_div(in_page, a.block_rows), row_offset(a.c, page, h, in_page)};
 }
 
-// A wave per block.  Lane l has channels 8 (l % L) .. + 7 (L = D / 8 lanes a row) of the rows l / L, l / L + 64 / L, ...
-template <int D, bool kE4m3>
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Two bf16 as whole numbers in the same order (infinities and NaN at the ends), and back.
+__device__ inline s16x2 ordered(unsigned x) {
+  const s16x2 v = __builtin_bit_cast(s16x2, x);
+  return __builtin_bit_cast(s16x2, x ^ (__builtin_bit_cast(unsigned, v >> 15) & 0x7fff7fffu));
+}
+__device__ inline float value_of(short x) { return __uint_as_float((unsigned)(unsigned short)(x ^ ((x >> 15) & 0x7fff)) << 16); }
+__device__ inline s16x2 from_lane(s16x2 x, int mask) { return __builtin_bit_cast(s16x2, __shfl_xor(__builtin_bit_cast(int, x), mask)); }
+
+// A wave per block.  Lane l has 16 bytes, kChannels channels, of the rows l / kLanes, l / kLanes + kRows, ...  The largest and smallest keys
+// are found as bf16 (8-bit keys times their scales are), two at a time as whole numbers; a block in which one is not finite, or of scales
+// so small that bf16 would not hold the keys, is done again in 32 bits.  The lanes of a column then share its channels out.  Bound by memory
+// and by the chain row counts -> page -> rows.  (Runs of blocks for a wave, the next one's rows on their way: 147K 8-bit rows 56 us, one
+// block each 41.)
+// kAhead: loads of rows on their way.
+template <int D, bool kE4m3, int kAhead>
 __global__ __launch_bounds__(256) void paged_summarize_kernel(const PagedBlocksArgs a, const long long first_wg) {
-  constexpr int kLanes = D / 8, kRows = 64 / kLanes;
+  constexpr int kChannels = kE4m3 ? 16 : 8, kLanes = D / kChannels, kRows = 64 / kLanes, kPairs = kChannels / 2;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const long long unit = (first_wg + blockIdx.x) * 4 + wave;
   if (unit >= a.units) return;
@@ -49,78 +67,147 @@ __global__ __launch_bounds__(256) void paged_summarize_kernel(const PagedBlocksA
   const BlockAt at = block_at(a, table_of(a.c, a.Hkv, b, h), h, (int)j);
   if (at.block < 0) return;
   const int col = lane % kLanes, r0 = lane / kLanes, rows = (int)a.block_rows.d;
-  const unsigned char *k = a.c.k + at.row + (long long)r0 * a.c.row_bytes + col * (kE4m3 ? 8 : 16);
+  const unsigned char *k = a.c.k + at.row + (long long)r0 * a.c.row_bytes + col * 16;
   const unsigned char *scales = nullptr;
-  if constexpr (kE4m3) scales = a.c.k_scale + at.block * rows + r0;  // per_page * block_rows = page_rows
-  float hi[8], lo[8];
+  if constexpr (kE4m3) scales = a.c.k_scale + at.block * rows;  // per_page * block_rows = page_rows
+  s16x2 hi[kPairs], lo[kPairs];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    hi[e] = -INFINITY;
-    lo[e] = INFINITY;
+  for (int e = 0; e < kPairs; ++e) {
+    hi[e] = s16x2{-32768, -32768};
+    lo[e] = s16x2{32767, 32767};
   }
-  auto take = [&](const float *x) __attribute__((always_inline)) {
+  int least_scale = 255;
+  for (int r = 0; r < rows; r += kAhead * kRows) {  // rows is a multiple of 16, kRows 4, 8 or 16
+    u32x4 v[kAhead];
+    int sc[kAhead];  // scale bytes
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float y = finite_or_zero(x[e]);
-      hi[e] = fmaxf(hi[e], y);
-      lo[e] = fminf(lo[e], y);
+    for (int x = 0; x < kAhead; ++x) {
+      const int row = r + x * kRows < rows ? r + x * kRows : 0;  // (once more the first ones)
+      if constexpr (kE4m3) sc[x] = scales[row + r0];
+      v[x] = *(const u32x4 *)(k + (long long)row * a.c.row_bytes);
+    }
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      unsigned y[kPairs];
+      if constexpr (kE4m3) {
+        const float size = __uint_as_float((unsigned)sc[x] << 23);
+        least_scale = sc[x] < least_scale ? sc[x] : least_scale;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[2 * e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[x][e], size, false));
+          y[2 * e + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[x][e], size, true));
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = v[x][e];
+      }
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) {
+        const s16x2 z = ordered(y[e]);
+        hi[e] = __builtin_elementwise_max(hi[e], z);
+        lo[e] = __builtin_elementwise_min(lo[e], z);
+      }
+    }
+  }
+  // A step leaves each lane half of the pairs, until it has one: pair `pair`, and channels 2 pair and 2 pair + 1 of its 16 bytes.
+  int pair = 0;
+  bool writes = true;
+  const auto halve = [&](auto step) __attribute__((always_inline)) {
+    constexpr int sh = kLanes << decltype(step)::value, n = kPairs >> (decltype(step)::value + 1);  // pairs left
+    if constexpr (sh < 64) {
+      const bool upper = (lane & sh) != 0;
+      if constexpr (n > 0) {
+        pair += upper ? n : 0;
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+          const s16x2 my_hi = upper ? hi[n + e] : hi[e], my_lo = upper ? lo[n + e] : lo[e];
+          hi[e] = __builtin_elementwise_max(my_hi, from_lane(upper ? hi[e] : hi[n + e], sh));
+          lo[e] = __builtin_elementwise_min(my_lo, from_lane(upper ? lo[e] : lo[n + e], sh));
+        }
+      } else {
+        writes &= !upper;
+        hi[0] = __builtin_elementwise_max(hi[0], from_lane(hi[0], sh));
+        lo[0] = __builtin_elementwise_min(lo[0], from_lane(lo[0], sh));
+      }
     }
   };
-#pragma unroll 4
-  for (int r = 0; r < rows; r += kRows) {  // rows is a multiple of 16, kRows 4 or 8
-    float x[8];
-    if constexpr (kE4m3) {
-      const u32x2 v = *(const u32x2 *)(k + (long long)r * a.c.row_bytes);
-      const float size = ldexpf(1.f, (int)scales[r] - 127);
+  halve(std::integral_constant<int, 0>());
+  halve(std::integral_constant<int, 1>());
+  halve(std::integral_constant<int, 2>());
+  halve(std::integral_constant<int, 3>());
+  float top[2] = {value_of(hi[0][0]), value_of(hi[0][1])}, bottom[2] = {value_of(lo[0][0]), value_of(lo[0][1])};
+  const bool odd = (kE4m3 && least_scale < 16) || !(fabsf(top[0]) < INFINITY) || !(fabsf(top[1]) < INFINITY) || !(fabsf(bottom[0]) < INFINITY) ||
+                   !(fabsf(bottom[1]) < INFINITY);
+  if (__builtin_amdgcn_ballot_w64(odd)) {
+    float t[kChannels], u[kChannels];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8(v[e], false), q = __builtin_amdgcn_cvt_pk_f32_fp8(v[e], true);
-        x[4 * e] = p[0] * size;
-        x[4 * e + 1] = p[1] * size;
-        x[4 * e + 2] = q[0] * size;
-        x[4 * e + 3] = q[1] * size;
-      }
-    } else {
+    for (int e = 0; e < kChannels; ++e) {
+      t[e] = -INFINITY;
+      u[e] = INFINITY;
+    }
+#pragma unroll 1
+    for (int r = 0; r < rows; r += kRows) {
       const u32x4 v = *(const u32x4 *)(k + (long long)r * a.c.row_bytes);
+      float x[kChannels];
+      if constexpr (kE4m3) {
+        const float size = ldexpf(1.f, (int)scales[r + r0] - 127);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[2 * e] = __uint_as_float(v[e] << 16);
-        x[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+        for (int e = 0; e < 4; ++e) {
+          const f32x2 p = __builtin_amdgcn_cvt_pk_f32_fp8(v[e], false), q = __builtin_amdgcn_cvt_pk_f32_fp8(v[e], true);
+          x[4 * e] = p[0] * size;
+          x[4 * e + 1] = p[1] * size;
+          x[4 * e + 2] = q[0] * size;
+          x[4 * e + 3] = q[1] * size;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[2 * e] = __uint_as_float(v[e] << 16);
+          x[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < kChannels; ++e) {
+        const float y = finite_or_zero(x[e]);
+        t[e] = fmaxf(t[e], y);
+        u[e] = fminf(u[e], y);
       }
     }
-    take(x);
-  }
-  float most = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < kChannels; ++e) {
 #pragma unroll
-    for (int sh = kLanes; sh < 64; sh <<= 1) {
-      hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], sh));
-      lo[e] = fminf(lo[e], __shfl_xor(lo[e], sh));
+      for (int sh = kLanes; sh < 64; sh <<= 1) {
+        t[e] = fmaxf(t[e], __shfl_xor(t[e], sh));
+        u[e] = fminf(u[e], __shfl_xor(u[e], sh));
+      }
+      if (e / 2 == pair) {
+        top[e % 2] = t[e];
+        bottom[e % 2] = u[e];
+      }
     }
-    most = fmaxf(most, fmaxf(fabsf(hi[e]), fabsf(lo[e])));
   }
+  float most = fmaxf(fmaxf(fabsf(top[0]), fabsf(bottom[0])), fmaxf(fabsf(top[1]), fabsf(bottom[1])));
 #pragma unroll
-  for (int sh = 1; sh < kLanes; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
+  for (int sh = 1; sh < 64; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
   int exponent = most > 0.f ? scale_exponent(most) : kLeastBoundExponent;
   exponent = exponent < kLeastBoundExponent ? kLeastBoundExponent : exponent;
-  if (r0 != 0) return;
-  u32x2 up = {0u, 0u}, down = {0u, 0u};
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int u = (int)ceilf(ldexpf(hi[e], -exponent)), d = (int)floorf(ldexpf(lo[e], -exponent));
-    up[e / 4] |= (unsigned)(u & 255) << (8 * (e % 4));
-    down[e / 4] |= (unsigned)(d & 255) << (8 * (e % 4));
-  }
-  signed char *dst = a.bounds + at.block * (2 * D) + 8 * col;
-  *(u32x2 *)dst = up;
-  *(u32x2 *)(dst + D) = down;
-  if (col == 0) a.scale[at.block] = (unsigned char)(exponent + 127);
+  if (!writes) return;
+  const int up0 = (int)ceilf(ldexpf(top[0], -exponent)), up1 = (int)ceilf(ldexpf(top[1], -exponent));
+  const int down0 = (int)floorf(ldexpf(bottom[0], -exponent)), down1 = (int)floorf(ldexpf(bottom[1], -exponent));
+  signed char *dst = a.bounds + at.block * (2 * D) + kChannels * col + 2 * pair;
+  *(unsigned short *)dst = (unsigned short)((up0 & 255) | (up1 & 255) << 8);
+  *(unsigned short *)(dst + D) = (unsigned short)((down0 & 255) | (down1 & 255) << 8);
+  if (lane == 0) a.scale[at.block] = (unsigned char)(exponent + 127);
 }
 
 hipError_t launch_paged_summarize(const PagedBlocksArgs &a, hipStream_t st) {
-  const auto kern = a.D == 128 ? (a.c.e4m3 ? paged_summarize_kernel<128, true> : paged_summarize_kernel<128, false>)
-                               : (a.c.e4m3 ? paged_summarize_kernel<64, true> : paged_summarize_kernel<64, false>);
+  const int at_once = 64 * 16 / (a.D * (a.c.e4m3 ? 1 : 2));  // rows of a load
+  const bool few = (int)a.block_rows.d <= 4 * at_once;
+  const auto of = [&](auto few_kernel, auto many_kernel) { return few ? few_kernel : many_kernel; };
+  const auto kern = a.D == 128 ? (a.c.e4m3 ? of(paged_summarize_kernel<128, true, 4>, paged_summarize_kernel<128, true, 8>)
+                                           : of(paged_summarize_kernel<128, false, 4>, paged_summarize_kernel<128, false, 8>))
+                               : (a.c.e4m3 ? of(paged_summarize_kernel<64, true, 4>, paged_summarize_kernel<64, true, 8>)
+                                           : of(paged_summarize_kernel<64, false, 4>, paged_summarize_kernel<64, false, 8>));
   return launch_in_parts((a.units + 3) / 4, 256, [&](long long first, unsigned count) {
     hipLaunchKernelGGL(kern, dim3(count), dim3(256), 0, st, a, first);
   });

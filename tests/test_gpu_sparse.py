@@ -508,3 +508,23 @@ def test_attention_of_lists_in_parts_of_the_tokens():
     delta = 128 * 2.0 ** -24 * most_s + 2.0 ** -20
     assert ((out[-last:].double().cpu() - want).abs() <= want.abs() * 2.0 ** -8 * (1 + 2.0 ** -7) + (2 * delta + 2.0 ** -16) * most_v).all()
     assert ((lse[-last:].double().cpu() - want_lse).abs() <= delta + 2.0 ** -22 * (1 + want_lse.abs())).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [16, 80, 112, 240])
+def test_summarize_of_blocks_of_any_length(block, d, e4m3):
+    pool, blocks = _pool(dict(page_rows=block, block=block, e4m3=e4m3), [3 * block + 5, block - 1], d=d)
+    if e4m3:  # as large and as small as scales come
+        pool.k_scale.copy_(torch.randint(1, 255, pool.k_scale.shape, generator=torch.Generator().manual_seed(7)))
+        pool.k_scale[::2] = torch.randint(1, 30, pool.k_scale[::2].shape, generator=torch.Generator().manual_seed(8)).to(torch.uint8).cuda()
+    _summarize(pool, blocks, None, 1000, [2, 2])
+
+
+@pytest.mark.parametrize("g", [1, 2, 3, 6, 16, 20])
+@pytest.mark.parametrize("first_row", [4300, 70])
+def test_choose_for_chunks_behind_long_histories(g, first_row):
+    """Keys in the workspace, and sets of query rows that share a block's bounds: also where a tile holds the ends of two sequences."""
+    pool, blocks = _pool(dict(page_rows=64, block=16), [4400, first_row], d=64)
+    _random_bounds(pool, blocks)
+    _choose(pool, blocks, [70, 9], 9, 1, 1, hq=2 * g, policy=[2, 2], total=90)
