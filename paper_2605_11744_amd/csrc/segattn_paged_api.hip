@@ -209,7 +209,7 @@ struct ReserveSpace {
 bool reserve_space(const Problem &p, const PagedCache &c, ReserveSpace &s) {
   if ((c.per_head ? (long long)p.Hkv : 1ll) * c.max_pages >= kMostRows) return false;
   s.chunks = ((long long)c.n_pages + kTablePages - 1) / kTablePages;
-  s.free_of = align_up(4ull * p.B);
+  s.free_of = align_up(4ull * p.B * (c.per_head ? p.Hkv : 1));
   s.free = align_up(s.free_of + 4ull * s.chunks);
   s.total = s.free + align_up(4ull * c.n_pages);
   return true;
@@ -512,6 +512,11 @@ segattn_status seg_kv_paged_reserve(const segattn_config *cfg, const segattn_pag
   a.total = total;
   a.newest = newest_only;
   a.chunks = (int)s.chunks;
+  a.heads_div = fast_div_by(p.Hkv);
+  a.longest = (int)max_seqlen;
+  // a row range of m rows meets (m + page_rows - 2) / page_rows + 1 entries at most
+  const long long entries = (max_seqlen + a.c.page_rows.d - 2) / a.c.page_rows.d + 1;
+  a.small = p.B <= 256 && a.c.n_pages <= (1 << 18) && total * p.Hkv <= 2560 && (long long)p.B * p.Hkv * entries <= kSmallReserve;
   return hip_status(launch_paged_reserve(a, (hipStream_t)stream));
 }
 

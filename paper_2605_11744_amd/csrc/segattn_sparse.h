@@ -15,13 +15,16 @@ struct PagedTablesArgs {
   const int *rows;
   int *granted;
   long long *slots;      // or nullptr
-  int *need;             // workspace: [B] entries that a sequence lacks (-1: its rows do not fit), then where its pages begin in `free`
+  int *need;             // workspace: [table rows] entries that each lacks (-1: the rows do not fit), then where its pages begin in `free`
   int *free_of;          // workspace: [chunks] free pages among kTablePages
   int *free;             // workspace: [n_pages] free pages, ascending
   long long total;
   int B, Hkv, newest, tail, chunks;
-  FastDiv seg;
+  int longest;           // most new tokens of a sequence
+  int small;             // by one workgroup
+  FastDiv seg, heads_div;
 };
+constexpr long long kSmallReserve = 4096;  // entries that one workgroup hands out
 hipError_t launch_paged_reserve(const PagedTablesArgs &a, hipStream_t st);
 hipError_t launch_paged_release(const PagedTablesArgs &a, hipStream_t st);
 
