@@ -114,8 +114,8 @@ __global__ __launch_bounds__(64 * kChosenWaves, 2) void paged_chosen_kernel(cons
 #pragma unroll
     for (int l = 0; l < NL; ++l) {
       const long long from_row = at[l / (NL / 2)] + (l % (NL / 2)) * (RPL * a.c.row_bytes);
-      nk[l] = *(const u32x4 *)(a.c.k + from_row + mine);
-      nv[l] = *(const u32x4 *)(a.c.v + from_row + mine);
+      nk[l] = __builtin_nontemporal_load((const u32x4 *)(a.c.k + from_row + mine));
+      nv[l] = __builtin_nontemporal_load((const u32x4 *)(a.c.v + from_row + mine));
     }
     if constexpr (kE4m3) {
       const long long at0 = of_lane(half_place, 2 * j), at1 = of_lane(half_place, 2 * j + 1);
@@ -280,49 +280,68 @@ __global__ __launch_bounds__(64 * kChosenWaves, 2) void paged_chosen_kernel(cons
   }
 }
 
-// A wave per query head whose window was shared out: its parts' partials joined.
+// A wave per (token, KV head) whose window was shared out, or (each = 1) per query head of it: the parts' partials joined, `each` query heads one
+// after the other.  (One sequence's 32 heads 4.3 us with a wave each and 10.4 with four a wave, a chunk of 2.5K tokens' 63 and 26.)
 template <int D>
-__global__ __launch_bounds__(256) void paged_chosen_join_kernel(const PagedChosenArgs a, const long long first_wg) {
-  constexpr int SF = D + kWsTailFloats, kLanes = D / 4, kGroups = 64 / kLanes;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const long long u = (first_wg + blockIdx.x) * 4 + wave;
-  if (u >= a.total * a.Hq) return;
-  const long long token = u / a.Hq;
-  const int head = (int)(u - token * a.Hq), h = head / a.g;
-  int hx = 0;  // h's place among the sets
-  while (a.head_of[hx] != h) ++hx;
+__global__ __launch_bounds__(256) void paged_chosen_join_kernel(const PagedChosenArgs a, const int hx0, const int heads, const int each, const long long first_wg) {
+  constexpr int SF = D + kWsTailFloats, kLanes = D / 4, kGroups = 64 / kLanes, kBatch = 4;
+  const int lane = threadIdx.x & 63;
+  const int turns = a.g / each;
+  const long long wave = (first_wg + blockIdx.x) * 4 + (threadIdx.x >> 6), u = wave / turns, token = u / heads;
+  if (token >= a.total) return;
+  const int j0 = (int)(wave - u * turns) * each;
+  const int hx = hx0 + (int)(u - token * heads), h = a.head_of[hx];
   const bool past = hx < a.n_past;
   const int parts = past ? a.parts_past : a.parts_other;
-  if (parts == 1) return;
   int i, n;
   if (sequence_of(a.cu, a.B, token, i, n) < 0) return;
-  const float *src = partial_of<D>(a, past, token, past ? hx : hx - a.n_past, 0) + (head - h * a.g) * SF;
-  const int d = lane % kLanes * 4;
-  float top = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = lane / kLanes; s < parts; s += kGroups) {
-    const float *part = src + (long long)s * a.g * SF;
-    const float2 ml = *(const float2 *)(part + D);
-    const f32x4 y = *(const f32x4 *)(part + d);
-    const float m_new = fmaxf(top, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
-    const float keep = __builtin_amdgcn_exp2f(top - ref), wgt = __builtin_amdgcn_exp2f(ml.x - ref);
-    l = l * keep + ml.y * wgt;
-    o = o * keep + y * wgt;
-    top = m_new;
+  const int group = lane / kLanes, d = lane % kLanes * 4;
+#pragma unroll 2
+  for (int j = j0; j < j0 + each; ++j) {
+    const float *src = partial_of<D>(a, past, token, past ? hx : hx - a.n_past, 0) + j * SF;
+    float top = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = group; s0 - group < parts; s0 += kGroups * kBatch) {
+      float2 ml[kBatch];
+      f32x4 y[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int s = s0 + kGroups * k;
+        const float *part = src + (long long)(s < parts ? s : parts - 1) * a.g * SF;
+        ml[k] = *(const float2 *)(part + D);
+        y[k] = *(const f32x4 *)(part + d);
+      }
+      float m_new = top;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (s0 + kGroups * k < parts) m_new = fmaxf(m_new, ml[k].x);
+      const float ref = m_new == -INFINITY ? 0.f : m_new, keep = __builtin_amdgcn_exp2f(top - ref);
+      l *= keep;
+      o *= keep;
+      top = m_new;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (s0 + kGroups * k < parts) {
+          const float wgt = __builtin_amdgcn_exp2f(ml[k].x - ref);
+          l += ml[k].y * wgt;
+          o += y[k] * wgt;
+        }
+      }
+    }
+    float most = top;
+#pragma unroll
+    for (int sh = kLanes; sh < 64; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
+    const float ref = most == -INFINITY ? 0.f : most, wgt = __builtin_amdgcn_exp2f(top - ref);
+    l *= wgt;
+    o *= wgt;
+#pragma unroll
+    for (int sh = kLanes; sh < 64; sh <<= 1) {
+      l += __shfl_xor(l, sh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], sh);
+    }
+    if (lane < kLanes) store_out<D>(a, token * a.Hq + h * a.g + j, d, o, l, ref);
   }
-  float most = top;
-#pragma unroll
-  for (int sh = kLanes; sh < 64; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
-  const float ref = most == -INFINITY ? 0.f : most, wgt = __builtin_amdgcn_exp2f(top - ref);
-  l *= wgt;
-  o *= wgt;
-#pragma unroll
-  for (int sh = kLanes; sh < 64; sh <<= 1) {
-    l += __shfl_xor(l, sh);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], sh);
-  }
-  if (lane < kLanes) store_out<D>(a, u, d, o, l, ref);
 }
 
 // Windows are shared out while there are fewer workgroups than two per compute unit of a 256-CU part, into parts of at least
@@ -410,9 +429,11 @@ static hipError_t launch_chosen(const PagedChosenArgs &a, hipStream_t st) {
   e = launch_in_parts(a.wgs_past + (a.wide_windows ? 0 : a.wgs_other), 64 * kChosenWaves, [&](long long first, unsigned count) {
     hipLaunchKernelGGL(kern, dim3(count), dim3(64 * kChosenWaves), 0, st, a, first);
   });
-  if (e != hipSuccess || (a.parts_past == 1 && a.parts_other == 1)) return e;
-  return launch_in_parts((a.total * a.Hq + 3) / 4, 256, [&](long long first, unsigned count) {
-    hipLaunchKernelGGL(paged_chosen_join_kernel<D>, dim3(count), dim3(256), 0, st, a, first);
+  const int hx0 = a.parts_past > 1 ? 0 : a.n_past, heads = (a.parts_other > 1 ? a.Hkv : a.n_past) - hx0;
+  if (e != hipSuccess || heads <= 0) return e;
+  const int each = a.total * heads < 8192 ? 1 : a.g;
+  return launch_in_parts((a.total * heads * (a.g / each) + 3) / 4, 256, [&](long long first, unsigned count) {
+    hipLaunchKernelGGL(paged_chosen_join_kernel<D>, dim3(count), dim3(256), 0, st, a, hx0, heads, each, first);
   });
 }
 

@@ -50,18 +50,23 @@ __global__ __launch_bounds__(256) void paged_count_kernel(const PagedChosenArgs 
   int u, e;
   const bool is = entry_of_thread(a, units, u, e);
   const int lane = threadIdx.x & 63, key = is ? entry_key(a, u, e, true) : -1;
-  int rank = -1;
+  // who counts for this lane, and its number among those it counts for
+  int leader = lane, before = 0, count = 1;
   unsigned long long left = __builtin_amdgcn_ballot_w64(key >= 0);
   for (int round = 0; round < 3 && left; ++round) {
-    const int leader = (int)__builtin_ctzll(left), theirs = __builtin_amdgcn_readlane(key, leader);
-    const unsigned long long same = __builtin_amdgcn_ballot_w64(key == theirs) & left;
-    int base = 0;
-    if (lane == leader) base = atomicAdd(a.counts + key, __popcll(same));
-    base = __builtin_amdgcn_readlane(base, leader);
-    if ((same >> lane) & 1) rank = base + __popcll(same & ((1ull << lane) - 1));
+    const int first = (int)__builtin_ctzll(left);
+    const unsigned long long same = __builtin_amdgcn_ballot_w64(key == __builtin_amdgcn_readlane(key, first)) & left;
+    if ((same >> lane) & 1) {
+      leader = first;
+      before = __popcll(same & ((1ull << lane) - 1));
+      count = __popcll(same);
+    }
     left &= ~same;
   }
-  if ((left >> lane) & 1) rank = atomicAdd(a.counts + key, 1);
+  int rank = 0;
+  if (key >= 0 && leader == lane) rank = atomicAdd(a.counts + key, count);
+  rank = __shfl(rank, leader) + before;
+  rank = key < 0 ? -1 : rank;
   if (is) a.rank[(long long)u * a.n_chosen + e] = rank;
 }
 // Places for every block's entries, and the workgroups' tasks: (key, first entry of it, entries).
@@ -558,12 +563,13 @@ __global__ __launch_bounds__(kListedThreads, 4) void paged_listed_kernel(const P
       if (base + 16 * g + col >= live) continue;
       const long long slot = ((long long)my_entry[g] * a.listed_pieces + sub) * a.g + my_head[g];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(a.listed_out + slot * D + 16 * nb + 4 * quad) = cols.O[g][nb];
+      for (int nb = 0; nb < NB; ++nb) __builtin_nontemporal_store(cols.O[g][nb], (f32x4 *)(a.listed_out + slot * D + 16 * nb + 4 * quad));
       if (quad == 0) a.listed_sum[slot] = float2{cols.m[g], l};
     }
   }
 }
 
+constexpr int kJoinBatch = 8;  // partials of half a wave under way together
 // A wave per query head of a PAST head: the partials of its token's entries.
 template <int D>
 __global__ __launch_bounds__(256) void paged_listed_join_kernel(const PagedChosenArgs a, const long long first_wg) {
@@ -596,12 +602,20 @@ __global__ __launch_bounds__(256) void paged_listed_join_kernel(const PagedChose
     unsigned long long there = __builtin_amdgcn_ballot_w64(e0 + lane < partials && (ml.x != -INFINITY || ml.y != 0.f));
     const float *src = a.listed_out + ((unit * partials + e0) * a.g + j) * D + d;
     const int most = min(64, partials - e0);
-#pragma unroll 8
-    for (int k = 0; k < most; k += kGroups) {
-      const int mine = k + group;
-      const bool is = mine < most && ((there >> mine) & 1);
-      const float w = __shfl(wgt, mine & 63);
-      if (is) o += *(const f32x4 *)(src + (long long)mine * a.g * D) * w;
+    for (int k0 = 0; k0 < most; k0 += kGroups * kJoinBatch) {
+      f32x4 y[kJoinBatch];
+      float w[kJoinBatch];
+#pragma unroll
+      for (int k = 0; k < kJoinBatch; ++k) {  // (no branches: the loads go together; of partials that are not there some other is read)
+        const int mine = k0 + kGroups * k + group;
+        const bool is = mine < most && ((there >> mine) & 1);
+        y[k] = __builtin_nontemporal_load((const f32x4 *)(src + (long long)(is ? mine : 0) * a.g * D));
+        w[k] = __shfl(wgt, mine & 63);
+        if (!is) y[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (!is) w[k] = 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < kJoinBatch; ++k) o += y[k] * w[k];
     }
   }
 #pragma unroll
