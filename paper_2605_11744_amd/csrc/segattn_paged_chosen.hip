@@ -6,6 +6,8 @@
 //   P = exp2((S^T - m) c)                 running maximum m and sum l per column, in fp32
 //   O^T[d][column] += V^T . P^T           A = V^T via ds_read_b64_tr_b16, B = P from the S^T registers
 // P enters as two bf16 (what that leaves is below 2^-16 of a weight), for fp32 outputs as three.
+#include <math.h>
+
 #include <type_traits>
 
 #include "segattn_paged_chosen.h"
@@ -344,12 +346,27 @@ __global__ __launch_bounds__(256) void paged_chosen_join_kernel(const PagedChose
   }
 }
 
-// Windows are shared out while there are fewer workgroups than two per compute unit of a 256-CU part, into parts of at least
-// two tiles per wave.
 constexpr long long kListedSpace = 1ull << 30;  // partials of listed blocks, of a token at least
-constexpr long long kListedLeast = 6, kPartTiles = 6;
+constexpr int kPartTiles = 6;
 constexpr long long kResident = 512;  // workgroups: two per compute unit of a 256-CU part
 constexpr int kListedColumns = 384;
+
+// Whether listed blocks are turned round and taken one by one, by how long both ways take (us).  Token by token: rounds of resident workgroups,
+// 32 rows of a wave at a time as they come from memory, or what all rows together need of the caches.  Block by block: the launches before and
+// behind, the partials written and read, and each row once.  Measured, both in us, eight KV heads of a 60K history in blocks of 64, 32 listed: 64
+// tokens of four query heads a KV head 66 and 76, 128 tokens 125 and 98, 400 tokens 388 and 155 (8-bit rows: 128 tokens 74 and 86, 400
+// tokens 222 and 137; heads of 64: 59 and 61, 176 and 94; one query head each: 64 tokens 66 and 64, 400 tokens 377 and 92); of an 8K history, 64
+// tokens 39 and 47, 128 tokens 73 and 65; two KV heads of eight query heads, 128 tokens 38 and 56, 400 tokens 114 and 84.
+bool blocks_one_by_one(const PagedChosenArgs &a, double parts, double tiles) {
+  const double row = 2.0 * a.D * (a.c.e4m3 ? 1 : 2), block = 16.0 * a.block_halves.d * row;
+  const double entries = (double)a.total * a.n_past * a.n_chosen, listed = entries * block, all = (double)a.B * a.n_past * a.blocks * block;
+  const double units = (double)a.total * a.n_past * a.passes * parts;
+  const double rounds = ceil(units / kResident) * ceil(tiles / kChosenWaves) * 3.2 * row / 512;
+  const double bytes = listed / (all <= 40e6 ? 14.5e6 : 8.5e6);
+  const double partials = entries * a.listed_pieces * a.g * (a.D + 2) * 4;
+  return 30 + (2 * partials + (listed < all ? listed : all)) / 5e6 < (rounds > bytes ? rounds : bytes);
+}
+
 unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, unsigned char *ws) {
   unsigned long long at = 0;
   const auto take = [&](auto *&x, unsigned long long count) {
@@ -361,19 +378,17 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
   a.wide_tokens = many ? kWideColumns / a.g : 1;
   a.listed_tokens = kListedColumns / a.g > 0 ? kListedColumns / a.g : 1;
   a.wide_windows = many && a.n_other > 0;
-  // Blocks are taken one by one where one is listed by several tokens of a sequence, as far as the host can tell.
   const int block_rows = 16 * (int)a.block_halves.d;
   a.blocks = (int)(((long long)a.max_rows + block_rows - 1) / block_rows);
   a.listed_pieces = (block_rows + kListedRows - 1) / kListedRows;
-  const double keys = (double)a.B * a.n_past * a.blocks, listed = (double)a.total * a.n_past * a.n_chosen;
-  a.by_block = many && a.n_past > 0 && keys < 1e9 && listed >= kListedLeast * keys && (double)a.n_past * a.n_chosen * a.listed_pieces < 1e8;
-  const long long units_past = a.by_block ? 0 : a.total * a.n_past * a.passes;
+  long long units_past = a.total * a.n_past * a.passes;
   const long long units_other = a.n_other * (a.wide_windows ? (a.cu ? a.total / a.wide_tokens + a.B : a.total) : a.total * a.passes);
   const long long halves = (long long)a.n_chosen * a.block_halves.d;
   long long window = (long long)a.seg.d + a.tail + a.wide_tokens;
   window = window < a.max_rows ? window : a.max_rows;
   const long long tiles_past = a.n_past ? (halves + 1) / 2 : 1, tiles_other = window / kChosenTile + 2;
   const long long units = units_past + (a.wide_windows ? 0 : units_other);
+  // Windows are shared out while there are fewer workgroups than two per compute unit of a 256-CU part.
   auto share = [&](long long tiles, long long p, long long least, int &parts, int &per_part) {
     const long long most = tiles / least;
     p = p < most ? p : most;
@@ -383,6 +398,8 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
   };
   const long long narrow = units >= kResident || units == 0 ? 1 : kResident / units;
   share(tiles_past, narrow, 2 * kChosenWaves, a.parts_past, a.tiles_past);
+  const double keys = (double)a.B * a.n_past * a.blocks;
+  a.by_block = many && a.n_past > 0 && keys < 1e9 && (double)a.n_past * a.n_chosen * a.listed_pieces < 1e8 && blocks_one_by_one(a, a.parts_past, a.tiles_past);
   // Windows that share their tiles: the parts that make the rounds of resident workgroups, times their length, shortest, where that is a
   // tenth or more.  A part costs as much as kPartTiles tiles to leave and to join.
   const auto rounds = [&](long long p) { return (units_other * p + kResident - 1) / kResident; };
@@ -395,7 +412,10 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
     }
   }
   share(tiles_other, a.wide_windows ? wide : narrow, a.wide_windows ? 16 : 2 * kChosenWaves, a.parts_other, a.tiles_other);
-  if (a.by_block) a.parts_past = 1;
+  if (a.by_block) {
+    a.parts_past = 1;
+    units_past = 0;
+  }
   a.wgs_past = units_past * a.parts_past;
   a.wgs_other = units_other * a.parts_other;
   unsigned long long slots = 0;

@@ -98,8 +98,8 @@ __global__ __launch_bounds__(256) void paged_sort_kernel(const PagedChosenArgs a
   int u, e;
   if (!entry_of_thread(a, units, u, e)) return;
   const long long entry = (long long)u * a.n_chosen + e;
-  const int rank = a.rank[entry];
-  if (rank >= 0) a.sorted[a.offsets[entry_key(a, u, e, false)] + rank] = (int)entry;
+  const int rank = a.rank[entry], key = rank < 0 ? -1 : entry_key(a, u, e, false);
+  if (key >= 0) a.sorted[a.offsets[key] + rank] = (int)entry;
 }
 
 // ---- arithmetic ------------------------------------------------------------------------------

@@ -182,12 +182,14 @@ def attention(pool, q, cu, rows, policy, seg, tail, lists, block_rows, scale=0.0
                 end = n - m + i + 1
                 end = max(0, min(end, max_rows) if max_rows else end)
                 if policy[h] & 2:
-                    see = [r for e in lists[t, past.index(h)].tolist() if e >= 0 for r in range(e * block_rows, min(end, (e + 1) * block_rows))]
+                    mine = lists[t, past.index(h)].to(torch.int64)
+                    see = (mine[mine >= 0][:, None] * block_rows + torch.arange(block_rows)).flatten()
+                    see = see[see < end]
                 else:
-                    see = list(range(ref.first_row(end, policy[h], seg, tail), end))
-                see = [r for r in see if ok[r]] if see else []
+                    see = torch.arange(ref.first_row(end, policy[h], seg, tail), end)
+                see = see[ok[see]] if len(see) else see
                 out[t, heads], lse[t, heads] = 0.0, -math.inf
-                if not see:
+                if not len(see):
                     continue
                 k, v = kk[see], vv[see]
                 odd[t, heads] = not bool(k.isfinite().all() and v.isfinite().all())

@@ -480,51 +480,79 @@ def test_attention_of_ragged_tokens_in_bf16(kind):
 
 def test_attention_of_lists_in_parts_of_the_tokens():
     """More partials than the workspace holds at a time: the tokens go in parts, to the same results as in calls of their own."""
-    pool, _ = _pool(dict(page_rows=256, block=16), [3300], hkv=1)
-    n, chosen, most = 2600, 64, pool.max_pages * pool.R
+    pool, _ = _pool(dict(page_rows=256, block=64), [9000], hkv=1)
+    n, chosen, most, hq = 8400, 72, pool.max_pages * pool.R, 4
     g = torch.Generator().manual_seed(8)
-    q = torch.randn((n, 16, 128), generator=g).to(BF16).cuda()
-    lists = torch.randint(0, 3300 // 16 + 2, (n, 1, chosen), generator=g).to(I32)
-    cfg, blocks = _cfg(pool, 16), sa.make_blocks(block_rows=16)
-    entry = 16 * (128 + 2) * 4  # bytes of an entry's partials
-    assert n * chosen * entry > sa.seg_attn_paged_chosen_workspace_bytes(cfg, pool.pages(), blocks, n, n, most, chosen) > 1000 * chosen * entry
+    q = torch.randn((n, hq, 128), generator=g).to(BF16).cuda()
+    lists = torch.randint(0, 9000 // 64 + 2, (n, 1, chosen), generator=g).to(I32)
+    cfg, blocks = _cfg(pool, hq), sa.make_blocks(block_rows=64)
+    entry = hq * (128 + 2) * 4  # bytes of an entry's partials
+    assert n * chosen * entry > sa.seg_attn_paged_chosen_workspace_bytes(cfg, pool.pages(), blocks, n, n, most, chosen) > 5000 * chosen * entry
 
     def call(first, count):
-        out, lse = torch.empty((count, 16, 128), dtype=BF16, device="cuda"), torch.empty((count, 16), device="cuda")
-        rows = torch.tensor([[3300 - (n - first - count)]], dtype=I32, device="cuda")
+        out, lse = torch.empty((count, hq, 128), dtype=BF16, device="cuda"), torch.empty((count, hq), device="cuda")
+        rows = torch.tensor([[9000 - (n - first - count)]], dtype=I32, device="cuda")
         need = sa.seg_attn_paged_chosen_workspace_bytes(cfg, pool.pages(), blocks, count, count, most, chosen)
+        assert need > count * chosen * entry or count == n
         ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
         sa.seg_attn_paged_chosen(cfg, pool.pages(), blocks, q[first:first + count].contiguous(), torch.tensor([0, count], dtype=I32, device="cuda"), count, count,
                                  rows, most, lists[first:first + count].cuda(), chosen, out, lse, ws, need, stream=_stream())
         return out, lse
 
     out, lse = call(0, n)
-    parts = [call(0, 900), call(900, 900), call(1800, 800)]
+    parts = [call(0, 3000), call(3000, 3000), call(6000, 2400)]
     assert torch.equal(out, torch.cat([p[0] for p in parts])) and torch.equal(lse, torch.cat([p[1] for p in parts]))
     # and the last tokens against the definition
     last = 5
-    pool.rows[0, 0] = 3300
-    want, want_lse, _, most_s, most_v = sref.attention(pool, q[-last:], [0, last], [[3300]], [2], 64, 16, lists[-last:], 16)
+    want, want_lse, _, most_s, most_v = sref.attention(pool, q[-last:], [0, last], [[9000]], [2], 64, 16, lists[-last:], 64)
     delta = 128 * 2.0 ** -24 * most_s + 2.0 ** -20
     assert ((out[-last:].double().cpu() - want).abs() <= want.abs() * 2.0 ** -8 * (1 + 2.0 ** -7) + (2 * delta + 2.0 ** -16) * most_v).all()
     assert ((lse[-last:].double().cpu() - want_lse).abs() <= delta + 2.0 ** -22 * (1 + want_lse.abs())).all()
 
 
+# Chunks so long that a listed block is taken once for all tokens that list it.
+def _long_chunk(kind, *, d=128, g=4, policy=(2, 3), chosen=8, new=(1290, 0, 17), held=(700, 30, 2000), seed=0):
+    lengths = [h + n for h, n in zip(held, new)]
+    pool, blocks = _pool(kind, lengths, d=d, hkv=len(policy), seed=seed)
+    total = sum(new) + 3
+    cfg, most = _cfg(pool, len(policy) * g, list(policy)), pool.max_pages * pool.R
+    need = sa.seg_attn_paged_chosen_workspace_bytes(cfg, pool.pages(), sa.make_blocks(block_rows=blocks.rows), total, max(new), most, chosen)
+    assert need > sum(new) * 2 * chosen * g * d * 4  # the partials of every entry
+    return pool, blocks.rows, list(new), total
+
+
+LONG = [dict(page_rows=64, block=64), dict(page_rows=128, block=128, per_head=True), dict(page_rows=96, block=48), dict(page_rows=80, block=80, token_major=True),
+        dict(page_rows=64, block=64, e4m3=True), dict(page_rows=128, block=64, e4m3=True, per_head=True)]
+
+
+@pytest.mark.parametrize("kind", LONG, ids=_name)
+@pytest.mark.parametrize("out_fp32", [False, True])
+def test_attention_of_long_chunks(kind, out_fp32):
+    chosen, g = (16, 2) if kind.get("e4m3") else (8, 4)
+    pool, block, new, total = _long_chunk(kind, chosen=chosen, g=g, **(dict(new=(2600, 0, 17)) if kind.get("e4m3") else {}))
+    _attend(pool, block, new, chosen, hq=2 * g, policy=[2, 3], out_fp32=out_fp32, total=total)
+
+
+@pytest.mark.parametrize("d,g", [(64, 1), (64, 8), (128, 3), (128, 1)])
+def test_attention_of_long_chunks_of_any_group(d, g):
+    chosen = 16 if g == 8 else 8
+    pool, block, new, total = _long_chunk(dict(page_rows=64, block=64), d=d, g=g, chosen=chosen, new=(2600, 0, 17) if g == 8 else (1290, 0, 17))
+    _attend(pool, block, new, chosen, hq=2 * g, policy=[2, 3], total=total)
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
-@pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("block", [16, 80, 112, 240])
-def test_summarize_of_blocks_of_any_length(block, d, e4m3):
-    pool, blocks = _pool(dict(page_rows=block, block=block, e4m3=e4m3), [3 * block + 5, block - 1], d=d)
-    if e4m3:  # as large and as small as scales come
-        pool.k_scale.copy_(torch.randint(1, 255, pool.k_scale.shape, generator=torch.Generator().manual_seed(7)))
-        pool.k_scale[::2] = torch.randint(1, 30, pool.k_scale[::2].shape, generator=torch.Generator().manual_seed(8)).to(torch.uint8).cuda()
-    _summarize(pool, blocks, None, 1000, [2, 2])
-
-
-@pytest.mark.parametrize("g", [1, 2, 3, 6, 16, 20])
-@pytest.mark.parametrize("first_row", [4300, 70])
-def test_choose_for_chunks_behind_long_histories(g, first_row):
-    """Keys in the workspace, and sets of query rows that share a block's bounds: also where a tile holds the ends of two sequences."""
-    pool, blocks = _pool(dict(page_rows=64, block=16), [4400, first_row], d=64)
-    _random_bounds(pool, blocks)
-    _choose(pool, blocks, [70, 9], 9, 1, 1, hq=2 * g, policy=[2, 2], total=90)
+def test_long_chunks_are_not_touched_by_rows_that_are_not_seen(e4m3):
+    """NaN in blocks that some tokens do not list, behind tokens' own rows in blocks that they do, in rows without a page."""
+    n, chosen, g = (2600, 16, 2) if e4m3 else (1400, 8, 4)
+    pool, block, new, total = _long_chunk(dict(page_rows=64, block=64, e4m3=e4m3), new=(n, 0, 0), held=(600, 0, 0), chosen=chosen, g=g)
+    for r in (70, 71, 900, 1203, 1255, 1999):
+        for h in range(2):
+            page, hh, i = pool.place(0, h, [r])
+            for x in (pool.k, pool.v):
+                x[page.cuda(), hh, i.cuda()] = 0x7F if e4m3 else math.nan
+    pool.table[0, 5] = -1
+    lists = _lists(pool, new, chosen, block, [2, 3], total=total)
+    own = (600 + torch.arange(n)) // 64
+    lists[:n, :, 0] = own[:, None].to(I32)
+    out, lse, odd = _attend(pool, block, new, chosen, hq=2 * g, policy=[2, 3], lists=lists, total=total)
+    assert not odd.all() and odd.any() and out[~odd].isfinite().all()
