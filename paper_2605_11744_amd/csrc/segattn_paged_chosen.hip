@@ -211,13 +211,10 @@ __global__ __launch_bounds__(64 * kChosenWaves, 2) void paged_chosen_kernel(cons
     }
   };
 
-  const int per_part = past ? a.tiles_past : a.tiles_other;
-  const int t_begin = part * per_part;
-  int t_end = t_begin + per_part;
-  {
-    const long long all = past ? ((long long)a.n_chosen * a.block_halves.d + 1) / 2 : to > 0 ? (to + kChosenTile - 1) / kChosenTile - from / kChosenTile : 0;
-    if (t_end > all) t_end = (int)all;
-  }
+  // A window is shared out evenly, in whole rounds of the waves; a list by its length.
+  const int all = past ? (int)(((long long)a.n_chosen * a.block_halves.d + 1) / 2) : to > 0 ? (to + kChosenTile - 1) / kChosenTile - from / kChosenTile : 0;
+  const int per_part = past ? a.tiles_past : ((all + parts - 1) / parts + kChosenWaves - 1) / kChosenWaves * kChosenWaves;
+  const int t_begin = min(part * per_part, all), t_end = min(t_begin + per_part, all);
   for (int t = t_begin + wave; t < t_end; t += 32 * kChosenWaves) {
     look_up(t);
     const int covered = min(32, (t_end - t + kChosenWaves - 1) / kChosenWaves);
@@ -411,7 +408,10 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
       shortest = length;
     }
   }
-  share(tiles_other, a.wide_windows ? wide : narrow, a.wide_windows ? 16 : 2 * kChosenWaves, a.parts_other, a.tiles_other);
+  // (windows are of all lengths up to the longest: twice as many, so that it is not waited for: 48 sequences of 8-bit rows 65 us with a workgroup each
+  // and 60 with four, 30 of them 44 and 43, eight 20 and 23)
+  const long long ragged = units >= kResident || units == 0 ? 1 : (kResident * 2 + units - 1) / units;
+  share(tiles_other, a.wide_windows ? wide : ragged, a.wide_windows ? 16 : 2 * kChosenWaves, a.parts_other, a.tiles_other);
   if (a.by_block) {
     a.parts_past = 1;
     units_past = 0;

@@ -380,7 +380,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
 
   // ---- tiles t_begin .. t_end - 1, those without a row left out
   const int all = to > 0 ? (to + kChosenTile - 1) / kChosenTile - from / kChosenTile : 0;
-  const int t_begin = part * a.tiles_other, t_end = min(t_begin + a.tiles_other, all);
+  const int per_part = (all + a.parts_other - 1) / a.parts_other, t_begin = min(part * per_part, all), t_end = min(t_begin + per_part, all);
   int buf = 0;
   for (int t = t_begin; t < t_end; t += 32) {
     look_up(t);
