@@ -511,13 +511,14 @@ segattn_status seg_kv_paged_evict(const segattn_config *cfg, const segattn_pages
 /* ---- paged cache: tables kept on the device ------------------------------------------------
  *
  * users: device int32 [n_pages], how many table entries name a page; a page is free where that is 0 or less.  The two
- * calls below keep it for the tables that they change: a program that lets a second table name a page adds 1, and a
+ * calls below keep it for the tables that they change, of at most 2^31 - 4097 entries a sequence: a program that lets a second table name a page adds 1, and a
  * program whose tables name pages before its first call sets it.  pages->table is written (its entries behind a
  * sequence's last row have to be unnamed, say -1, where pages are wanted: a named one is taken to be reserved
  * already).  Both are in stream order and depend on nothing but their inputs. */
 
 /* Pages for tokens that are going to be appended: m of sequence b, cu_seqlens, total and max_seqlen as for
- * seg_kv_paged_append (there may be fewer tokens than total: cu_seqlens[B] <= total).  Head h wants the entries of rows rows[b,h] ..
+ * seg_kv_paged_append (there may be fewer tokens than total: cu_seqlens[B] <= total; total may be 0 with cu_seqlens, and is
+ * at most B * max_seqlen).  Head h wants the entries of rows rows[b,h] ..
  * rows[b,h] + m - 1, or (newest_only = 1) of those of them that the newest token sees under the head's policy.
  * Wanted entries that name no page are counted sequence by sequence (with per_head: head by head in it); a
  * sequence is granted its pages if it needs none, or if the free pages are enough for it and all sequences before it
@@ -546,10 +547,12 @@ segattn_status seg_kv_paged_release(const segattn_config *cfg, const segattn_pag
  * block_rows consecutive rows of a (sequence, KV head), and what it promises a query is bounded from the upper and
  * lower bounds of its keys in every channel.  Only PAST heads have blocks; the others keep their windows.  One token or many
  * per sequence: cu_seqlens, total and max_seqlen as for seg_kv_paged_append (cu_seqlens[B] <= total; what belongs to the
- * tokens from cu_seqlens[B] on is neither read nor written), and the tokens' rows have been appended: token i of
+ * tokens from cu_seqlens[B] on is neither read nor written; total may be 0 with cu_seqlens, the arrays of tokens may then be NULL, and
+ * is at most B * max_seqlen), and the tokens' rows have been appended: token i of
  * the m of sequence b is row r = rows[b,h] - m + i of head h, and sees no row behind its own.  max_rows (host, <= max_pages *
  * page_rows): the most rows of a head; it sizes launches and workspaces, and of a head that holds more only the first
- * max_rows are seen.  At most 128 query heads per KV head. */
+ * max_rows are seen.  At most 128 query heads per KV head.  What a call writes, its workspace among it, shares no byte with its other
+ * arrays (SEGATTN_EINVAL; of the pool's K and V the caller sees to that). */
 typedef struct {
   int32_t block_rows;     /* a multiple of 16 that divides page_rows; 64 is a good size           */
   int8_t *bounds;         /* device, 16-byte aligned, [n_pages][heads][page_rows / block_rows][2][D]: upper, then lower
@@ -576,7 +579,8 @@ segattn_status seg_kv_paged_summarize(const segattn_config *cfg, const segattn_p
  * q8 = q / 2^e, to nearest even, e the smallest exponent with |q| <= 127 * 2^e for all of them (elements that are not finite
  * count as 0), block j's score is
  *     2^(scale_j - 127) * max over the group of sum over channels of q8 * (q8 > 0 ? upper_j : lower_j),
- * formed and compared exactly: an upper bound of the block's largest score but for the rounding of q.  A block without a page has the lowest score.
+ * formed and compared exactly for scales as seg_kv_paged_summarize writes them: an upper bound of the block's largest score but for the
+ * rounding of q.  A block without a page has the lowest score.
  * workspace: device, >= ..._workspace_bytes() (0: invalid arguments), 256-byte aligned, overwritten: calls that may overlap need one each. */
 size_t seg_kv_paged_choose_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
                                            const segattn_blocks *blocks, int64_t total, int64_t max_rows,
@@ -588,7 +592,7 @@ segattn_status seg_kv_paged_choose(const segattn_config *cfg, const segattn_page
                                    void *workspace, size_t workspace_bytes, void *stream);
 
 /* Attention of the tokens q [total,Hq,D] (bf16): a query head of a PAST KV head sees the rows up to its token's own
- * in the n_chosen (1 .. 65536) listed blocks (chosen as above or the caller's own, in any order: an entry below 0 or behind the
+ * in the n_chosen (1 .. 65536, n_chosen * block_rows < 2^31 - 4096) listed blocks (chosen as above or the caller's own, in any order: an entry below 0 or behind the
  * token's block is no block, one that is listed twice counts twice); of another KV head the rows of the token's
  * window, max(0, s - T) (TAIL) or s up to its own, s the start of its segment.  out [total,Hq,D] bf16 or fp32 (cfg->out_fp32), lse
  * [total,Hq]; rows without a page are not seen, and a query head that sees no row has zeros and -infinity; one that

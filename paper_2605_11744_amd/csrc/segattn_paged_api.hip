@@ -181,7 +181,7 @@ template <size_t kOuts, size_t kIns>
 bool shared_bytes(const Bytes (&outs)[kOuts], const Bytes (&ins)[kIns]) {
   const auto meet = [](const Bytes &x, const Bytes &y) {
     const unsigned __int128 from_x = (uintptr_t)x.at, from_y = (uintptr_t)y.at;
-    return x.at && y.at && from_x < from_y + y.count && from_y < from_x + x.count;
+    return x.at && y.at && x.count && y.count && from_x < from_y + y.count && from_y < from_x + x.count;
   };
   for (size_t i = 0; i < kOuts; ++i) {
     for (size_t j = 0; j < i; ++j)
@@ -196,9 +196,13 @@ unsigned long long table_entries(const Problem &p, const PagedCache &c) {
   return (unsigned long long)p.B * (c.per_head ? p.Hkv : 1) * c.max_pages;
 }
 
-// A packed batch as the paged operators take it.
+// A packed batch of new tokens; one without any is a batch too.
+bool batch_size_fits(const Problem &p, int64_t total, int64_t max_seqlen) {
+  if (max_seqlen < 1 || max_seqlen >= kMostRows) return false;
+  return total == 0 || (total >= max_seqlen && total < kMostRows && total <= (long long)p.B * max_seqlen);
+}
 bool batch_fits(const Problem &p, const int32_t *cu_seqlens, int64_t total, int64_t max_seqlen) {
-  if (max_seqlen < 1 || total < max_seqlen || total >= kMostRows || total > (long long)p.B * max_seqlen) return false;
+  if (!batch_size_fits(p, total, max_seqlen)) return false;
   return cu_seqlens ? !misaligned(cu_seqlens, 4) : total == p.B && max_seqlen == 1;
 }
 
@@ -246,7 +250,7 @@ constexpr long long kMostChosen = 4096, kMostListed = 65536;
 constexpr unsigned long long kChoiceSpace = 256ull << 20;  // keys of as many tokens as fit are formed at a time, of one at least
 bool choose_space(const Problem &p, const PagedBlocksArgs &k, int64_t total, int64_t max_rows, int32_t n_chosen, PagedChooseArgs &a,
                   unsigned long long &bytes) {
-  if (p.n_past == 0 || p.g > kPagedMostGroup || total < 1 || total >= kMostRows || max_rows < 1 || max_rows > k.c.cap) return false;
+  if (p.n_past == 0 || p.g > kPagedMostGroup || total < 0 || total >= kMostRows || max_rows < 1 || max_rows > k.c.cap) return false;
   if (n_chosen < 1 || n_chosen > kMostChosen) return false;
   a.stride = (max_rows + k.block_rows.d - 1) / k.block_rows.d;
   const unsigned long long per_token = 4ull * p.n_past * a.stride;
@@ -254,6 +258,7 @@ bool choose_space(const Problem &p, const PagedBlocksArgs &k, int64_t total, int
   part = part < 16 ? 16 : part;
   a.part = (int)(part < (unsigned long long)total ? part : total);
   bytes = align_up(a.part * per_token);
+  bytes = bytes ? bytes : kAlign;
   return true;
 }
 
@@ -286,7 +291,7 @@ bool chosen_space(const Problem &p, const PagedCache &c, const segattn_blocks *b
     a.head_of[i] = (unsigned char)p.order[i];
     a.tail_of[i] = (p.policy[p.order[i]] & SEGATTN_TAIL) != 0;
   }
-  bytes = align_up(plan_paged_chosen(a, max_seqlen, (unsigned char *)ws));
+  bytes = total == 0 ? 0 : align_up(plan_paged_chosen(a, max_seqlen, (unsigned char *)ws));
   bytes = bytes ? bytes : kAlign;
   return true;
 }
@@ -579,12 +584,13 @@ segattn_status seg_kv_paged_choose(const segattn_config *cfg, const segattn_page
   if (!build_paged(cfg, p) || !build_pages(pages, p, c) || !build_blocks(blocks, p, c, true, a.k)) return SEGATTN_EINVAL;
   if (!batch_fits(p, cu_seqlens, total, max_seqlen) || !choose_space(p, a.k, total, max_rows, n_chosen, a, bytes)) return SEGATTN_EINVAL;
   if (keep_first < 0 || keep_recent < 1 || keep_first > n_chosen - keep_recent || keep_recent > n_chosen) return SEGATTN_EINVAL;
-  if (!q || !rows || !chosen || !workspace || workspace_bytes < bytes) return SEGATTN_EINVAL;
+  if ((total > 0 && (!q || !chosen)) || !rows || !workspace || workspace_bytes < bytes) return SEGATTN_EINVAL;
   if (misaligned(q, 16) || misaligned(rows, 4) || misaligned(chosen, 4) || misaligned(workspace, kAlign) || foreign(stream)) return SEGATTN_EINVAL;
   const Bytes outs[] = {{chosen, 4ull * total * p.n_past * n_chosen}, {workspace, bytes}};
   const Bytes ins[] = {{q, 2ull * total * p.Hq * p.D}, {rows, 4ull * p.B * p.Hkv}, {cu_seqlens, 4ull * (p.B + 1ull)},
                        {pages->table, 4 * table_entries(p, c)}, bounds_bytes(a.k), scale_bytes(a.k)};
   if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+  if (total == 0) return SEGATTN_OK;
   a.q = (const unsigned short *)q;
   a.cu = cu_seqlens;
   a.k.rows = rows;
@@ -609,7 +615,7 @@ size_t seg_attn_paged_chosen_workspace_bytes(const segattn_config *cfg, const se
   unsigned long long without, with;
   memset(&a, 0, sizeof(a));
   if (!build_paged(cfg, p) || !build_pages(pages, p, c)) return 0;
-  if (max_seqlen < 1 || total < max_seqlen || total >= kMostRows || total > (long long)p.B * max_seqlen) return 0;
+  if (!batch_size_fits(p, total, max_seqlen)) return 0;
   // (the call may come with cu_seqlens or, for one token of every sequence, without)
   if (!chosen_space(p, c, blocks, nullptr, total, max_seqlen, max_rows, n_chosen, nullptr, a, without)) return 0;
   if (!chosen_space(p, c, blocks, (const int32_t *)4, total, max_seqlen, max_rows, n_chosen, nullptr, a, with)) return 0;
@@ -627,7 +633,7 @@ segattn_status seg_attn_paged_chosen(const segattn_config *cfg, const segattn_pa
   memset(&a, 0, sizeof(a));
   if (!build_paged(cfg, p) || !build_pages(pages, p, c) || !batch_fits(p, cu_seqlens, total, max_seqlen)) return SEGATTN_EINVAL;
   if (!chosen_space(p, c, blocks, cu_seqlens, total, max_seqlen, max_rows, n_chosen, workspace, a, bytes)) return SEGATTN_EINVAL;
-  if (!q || !rows || !out || !lse || !workspace || workspace_bytes < bytes || (p.n_past && !chosen)) return SEGATTN_EINVAL;
+  if ((total > 0 && (!q || !out || !lse || (p.n_past && !chosen))) || !rows || !workspace || workspace_bytes < bytes) return SEGATTN_EINVAL;
   if (misaligned(q, 16) || misaligned(rows, 4) || misaligned(chosen, 4) || misaligned(out, p.out_fp32 ? 4 : 2) || misaligned(lse, 4) ||
       misaligned(workspace, kAlign) || foreign(stream))
     return SEGATTN_EINVAL;
@@ -636,6 +642,7 @@ segattn_status seg_attn_paged_chosen(const segattn_config *cfg, const segattn_pa
   const Bytes ins[] = {{q, heads * p.D * 2}, {rows, 4ull * p.B * p.Hkv}, {cu_seqlens, 4ull * (p.B + 1ull)},
                        {p.n_past ? chosen : nullptr, 4ull * total * p.n_past * n_chosen}, {pages->table, 4 * table_entries(p, c)}};
   if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+  if (total == 0) return SEGATTN_OK;
   a.q = (const unsigned short *)q;
   a.rows = rows;
   a.chosen = chosen;

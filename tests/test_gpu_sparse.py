@@ -126,6 +126,20 @@ def test_reserve_leaves_tokens_behind_the_last_sequence_and_finds_reserved_pages
     assert again[0].tolist() == want[0].tolist() and again[2] == [1, 1]
 
 
+@pytest.mark.parametrize("n_pages", [40, 1 << 19])
+def test_reserve_for_a_batch_without_tokens_grants_and_changes_nothing(n_pages):
+    """Either way of reserving: by one workgroup, and by launches for many pages."""
+    t = Tables(rows=[[5, 9, 0], [200, 0, 0]], page_rows=16, max_pages=16, policy=P3, n_pages=n_pages)
+    pages, cfg = t.device(), _cfg(t, t.H, P3)
+    granted = torch.full((2,), -9, dtype=I32, device="cuda")
+    need = sa.seg_kv_paged_reserve_workspace_bytes(cfg, pages)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    sa.seg_kv_paged_reserve(cfg, pages, t.u, torch.zeros(3, dtype=I32, device="cuda"), 0, 1, torch.tensor(t.rows, dtype=I32, device="cuda"), granted,
+                            torch.empty((0, 3), dtype=I64, device="cuda"), ws, need, stream=_stream())
+    assert granted.tolist() == [1, 1]
+    assert torch.equal(t.u.cpu(), t.users) and torch.equal(t.t.cpu(), t.table)
+
+
 def test_reserve_over_many_chunks_of_pages():
     t = Tables(rows=[[0, 0, 0]] * 9, page_rows=4, max_pages=1400, policy=[2, 2, 2], n_pages=40000, per_head=True)
     t.users[torch.rand(40000, generator=torch.Generator().manual_seed(3)) < 0.7] = 1
@@ -538,6 +552,44 @@ def test_attention_of_long_chunks_of_any_group(d, g):
     chosen = 16 if g == 8 else 8
     pool, block, new, total = _long_chunk(dict(page_rows=64, block=64), d=d, g=g, chosen=chosen, new=(2600, 0, 17) if g == 8 else (1290, 0, 17))
     _attend(pool, block, new, chosen, hq=2 * g, policy=[2, 3], total=total)
+
+
+def test_long_chunks_repeat_bit_for_bit_and_replay():
+    """The order in which listed blocks' entries are gathered is not that of the results; two graphs with a workspace each, lists that change."""
+    chosen, g = 8, 4
+    pool, block, new, total = _long_chunk(dict(page_rows=64, block=64), chosen=chosen, g=g)
+    cfg, blocks, most = _cfg(pool, 2 * g, [2, 3]), sa.make_blocks(block_rows=block), pool.max_pages * pool.R
+    q = torch.randn((total, 2 * g, 128), generator=torch.Generator().manual_seed(8)).to(BF16).cuda()
+    cu = torch.tensor(_sums(new), dtype=I32, device="cuda")
+    need = sa.seg_attn_paged_chosen_workspace_bytes(cfg, pool.pages(), blocks, total, max(new), most, chosen)
+    lists = _lists(pool, new, chosen, block, [2, 3], total=total).cuda()
+    sides = [(torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda"), torch.zeros((total, 2 * g, 128), device="cuda").to(BF16),
+              torch.zeros((total, 2 * g), device="cuda")) for _ in range(3)]
+
+    def call(ws, out, lse):
+        sa.seg_attn_paged_chosen(cfg, pool.pages(), blocks, q, cu, total, max(new), pool.rows, most, lists, chosen, out, lse, ws, need, stream=_stream())
+
+    call(*sides[0])
+    torch.cuda.synchronize()
+    graphs = []
+    for side in sides[1:]:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(*side)
+    for i in range(4):
+        lists.copy_(_lists(pool, new, chosen, block, [2, 3], seed=20 + i, total=total))
+        call(*sides[0])
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        for graph, s in zip(graphs, streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for side in sides[1:]:
+            assert torch.equal(side[1], sides[0][1]) and torch.equal(side[2], sides[0][2])
+        before = [x.clone() for x in sides[0][1:]]
+        call(*sides[0])
+        assert all(torch.equal(x, y) for x, y in zip(before, sides[0][1:]))
 
 
 @pytest.mark.parametrize("e4m3", [False, True])

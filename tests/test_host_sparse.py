@@ -63,7 +63,7 @@ def test_configurations_without_a_paged_form_are_refused(bad):
     _refused(attend, cfg)
 
 
-BATCHES = [dict(total=0), dict(longest=0), dict(total=4), dict(total=11), dict(total=1 << 31, longest=1 << 30), dict(cu=None), dict(cu=P + 2),
+BATCHES = [dict(total=-1), dict(total=0, cu=None), dict(total=0, longest=0), dict(total=0, longest=1 << 31), dict(longest=0), dict(total=4), dict(total=11), dict(total=1 << 31, longest=1 << 30), dict(cu=None), dict(cu=P + 2),
            dict(cu=None, total=2, longest=2)]
 
 
@@ -153,7 +153,7 @@ def test_attention_refuses_heads_and_lists_beyond_31_bits():
     pg = pages(page_rows=1 << 16, max_pages=1 << 10)
     assert sa.seg_attn_paged_chosen_workspace_bytes(_cfg(), pg, blocks(block_rows=1 << 16), 9, 5, 128, 30000) > 0
     assert sa.seg_attn_paged_chosen_workspace_bytes(_cfg(), pg, blocks(block_rows=1 << 16), 9, 5, 128, 32768) == 0
-    for total, longest in ((0, 1), (9, 0), (9, 4), (4, 5)):
+    for total, longest in ((-1, 1), (0, 0), (9, 0), (9, 4), (4, 5)):
         assert sa.seg_attn_paged_chosen_workspace_bytes(_cfg(), pages(), blocks(), total, longest, 128, 4) == 0
 
 
@@ -162,6 +162,20 @@ def test_a_step_of_one_sequence_has_room_for_its_parts():
     need = sa.seg_attn_paged_chosen_workspace_bytes(cfg, pg, blocks(), 1, 1, 1 << 17, 256)
     assert need > 8 * (128 + 2) * 4
     _refused(attend, cfg, pg, total=1, longest=1, cu=None, most=1 << 17, n=256, bytes=need - 1)
+
+
+def test_a_batch_without_tokens_has_nothing_to_be_done():
+    """Choice and attention then write nothing, and need nothing of what belongs to tokens; what else is refused still is."""
+    assert sa.seg_kv_paged_choose_workspace_bytes(_cfg(), pages(), blocks(), 0, 128, 4) > 0
+    need = sa.seg_attn_paged_chosen_workspace_bytes(_cfg(), pages(), blocks(), 0, 5, 128, 4)
+    assert need > 0
+    choose(total=0, q=None, chosen=None)
+    attend(total=0, q=None, chosen=None, out=None, lse=None, bytes=need)
+    choose(total=0, q=R, chosen=T)  # an array of no elements shares nothing
+    attend(total=0, out=T, lse=R)
+    for bad in (dict(rows=None), dict(ws=None), dict(most=129), dict(bytes=0), dict(ws=T)):
+        _refused(choose, total=0, **bad)
+        _refused(attend, total=0, **bad)
 
 
 def test_structure_has_the_layout_of_the_header():
