@@ -344,7 +344,6 @@ __global__ __launch_bounds__(256) void paged_chosen_join_kernel(const PagedChose
 }
 
 constexpr long long kListedSpace = 1ull << 30;  // partials of listed blocks, of a token at least
-constexpr int kPartTiles = 6;
 constexpr long long kResident = 512;  // workgroups: two per compute unit of a 256-CU part
 constexpr int kListedColumns = 384;
 
@@ -375,11 +374,12 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
   a.wide_tokens = many ? kWideColumns / a.g : 1;
   a.listed_tokens = kListedColumns / a.g > 0 ? kListedColumns / a.g : 1;
   a.wide_windows = many && a.n_other > 0;
+  a.wide_tiles = a.cu ? a.total / a.wide_tokens + a.B : a.total;
   const int block_rows = 16 * (int)a.block_halves.d;
   a.blocks = (int)(((long long)a.max_rows + block_rows - 1) / block_rows);
   a.listed_pieces = (block_rows + kListedRows - 1) / kListedRows;
   long long units_past = a.total * a.n_past * a.passes;
-  const long long units_other = a.n_other * (a.wide_windows ? (a.cu ? a.total / a.wide_tokens + a.B : a.total) : a.total * a.passes);
+  const long long units_other = a.n_other * (a.wide_windows ? a.wide_tiles : a.total * a.passes);
   const long long halves = (long long)a.n_chosen * a.block_halves.d;
   long long window = (long long)a.seg.d + a.tail + a.wide_tokens;
   window = window < a.max_rows ? window : a.max_rows;
@@ -397,21 +397,10 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
   share(tiles_past, narrow, 2 * kChosenWaves, a.parts_past, a.tiles_past);
   const double keys = (double)a.B * a.n_past * a.blocks;
   a.by_block = many && a.n_past > 0 && keys < 1e9 && (double)a.n_past * a.n_chosen * a.listed_pieces < 1e8 && blocks_one_by_one(a, a.parts_past, a.tiles_past);
-  // Windows that share their tiles: the parts that make the rounds of resident workgroups, times their length, shortest, where that is a
-  // tenth or more.  A part costs as much as kPartTiles tiles to leave and to join.
-  const auto rounds = [&](long long p) { return (units_other * p + kResident - 1) / kResident; };
-  long long wide = 1, shortest = rounds(1) * tiles_other * 9 / 10;
-  for (long long p = 2; a.wide_windows && p <= 8; ++p) {
-    const long long length = rounds(p) * ((tiles_other + p - 1) / p + kPartTiles);
-    if (length < shortest) {
-      wide = p;
-      shortest = length;
-    }
-  }
   // (windows are of all lengths up to the longest: twice as many, so that it is not waited for: 48 sequences of 8-bit rows 65 us with a workgroup each
   // and 60 with four, 30 of them 44 and 43, eight 20 and 23)
   const long long ragged = units >= kResident || units == 0 ? 1 : (kResident * 2 + units - 1) / units;
-  share(tiles_other, a.wide_windows ? wide : ragged, a.wide_windows ? 16 : 2 * kChosenWaves, a.parts_other, a.tiles_other);
+  share(tiles_other, a.wide_windows ? 1 : ragged, 2 * kChosenWaves, a.parts_other, a.tiles_other);
   if (a.by_block) {
     a.parts_past = 1;
     units_past = 0;
@@ -422,6 +411,19 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
   if (a.parts_past > 1) slots += (unsigned long long)a.total * a.n_past * a.parts_past;
   if (a.parts_other > 1) slots += (unsigned long long)a.total * a.n_other * a.parts_other;
   take(a.slots, slots * a.g * ws_slot_floats(a.D));
+  if (a.wide_windows) {
+    // Shares of equal length for as many workgroups as are resident (D = 64: three on a compute unit), but where the units alone are several
+    // rounds of them, a workgroup for each (8 heads with windows up to 5K, new tokens: 2048 342 us in shares and 449 by units,
+    // 8192 1041 and 1039, 16384 2105 and 2018).
+    const long long resident = a.D == 128 ? kResident : kResident * 3 / 2;
+    a.wide_wgs = 0;
+    if (units_other < 4 * resident) {
+      const long long most = units_other * (2 * tiles_other + kUnitTiles) / kLeastShare + 1;
+      a.wide_wgs = (int)(most < resident ? (most + 7) / 8 * 8 : resident);
+    }
+    take(a.splits, a.wide_wgs);
+    take(a.wide_slots, 2ll * a.wide_wgs * kWideColumns * ws_slot_floats(a.D));
+  }
   if (a.by_block) {
     const long long per_token = (long long)a.n_past * a.n_chosen;  // < 2^23
     long long part = kListedSpace / (per_token * a.listed_pieces * a.g * (a.D + 2) * 4);

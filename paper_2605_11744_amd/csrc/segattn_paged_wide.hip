@@ -268,7 +268,105 @@ __device__ __attribute__((always_inline)) bool stage_piece(unsigned char *dst, i
 }
 
 // ---- windows ---------------------------------------------------------------------------------
-template <int D, bool kE4m3, bool kFp32>
+// A unit: the heads of wide_tokens neighbouring tokens in one window; its tiles are those that one of the tokens sees.
+struct WindowUnit {
+  int x, b, i, n, tokens;  // the head of the set; sequence (-1: none), first token in it, its tokens; tokens of the unit
+  int all, some;           // tiles; the first ones, which only some of the tokens see (behind the start of a segment in the unit's middle)
+  int cost;                // in tiles: those of `some` count one and a half times (their masks, and a look for values that are not finite)
+  __device__ int tile_at(int at) const {  // the first tile of a piece that begins at `at`
+    at = max(at - kUnitTiles, 0);
+    return at < some + some / 2 ? at * 2 / 3 : at - some / 2;
+  }
+};
+__device__ inline WindowUnit window_unit(const PagedChosenArgs &a, long long u) {
+  WindowUnit r;
+  r.x = (int)(u / a.wide_tiles);
+  r.b = tile_of(a, u - r.x * a.wide_tiles, a.wide_tokens, r.i, r.n);
+  r.tokens = r.all = r.some = r.cost = 0;
+  if (r.b < 0) return r;
+  r.tokens = min(a.wide_tokens, r.n - r.i);
+  const int hx = a.n_past + r.x;
+  const long long w = (long long)r.b * a.Hkv + a.head_of[hx];
+  int from, last_from, to;
+  token_window(a, w, hx, r.i, r.n, from, to);
+  token_window(a, w, hx, r.i + r.tokens - 1, r.n, last_from, to);
+  r.all = to > 0 ? (to + kChosenTile - 1) / kChosenTile - from / kChosenTile : 0;
+  r.some = min((last_from + kChosenTile - 1) / kChosenTile - from / kChosenTile, r.all);
+  r.cost = kUnitTiles + r.all + r.some / 2;
+  return r;
+}
+// The units' tiles, one unit after the other, are cut into shares of one length, a workgroup each: windows are of all lengths, and with a
+// workgroup for each of them, or for halves, the part waits for the longest (2500 tokens, four heads with windows up to 5K: 281 us and 26 to
+// join in halves, 200 and 17 in shares).  Each workgroup finds its own: the threads sum up the units' costs, then lanes search the units
+// of the thread in whose sum the share begins.
+struct WindowShare {
+  long long unit, at;     // the first unit, and where it begins in the order of all tiles
+  long long begin, end;   // of the share
+  long long length;
+};
+__device__ inline WindowShare window_share(const PagedChosenArgs &a, long long index) {
+  __shared__ long long sm_sum[kWideThreads / 64], sm_start[2];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const long long units = a.wgs_other, each = (units + kWideThreads - 1) / kWideThreads;
+  long long sum = 0;
+  for (long long u = tid * each; u < min(units, (tid + 1) * each); ++u) sum += window_unit(a, u).cost;
+  long long before = sum;
+#pragma unroll
+  for (int sh = 1; sh < 64; sh <<= 1) {
+    const long long up = __shfl_up(before, sh);
+    if (lane >= sh) before += up;
+  }
+  if (lane == 63) sm_sum[wave] = before;
+  before -= sum;
+  __syncthreads();
+  long long all = 0;
+  for (int y = 0; y < kWideThreads / 64; ++y) {
+    if (y < wave) before += sm_sum[y];
+    all += sm_sum[y];
+  }
+  all = of_lane(all, 0);  // (the same in all lanes: scalar registers)
+  WindowShare s;
+  s.length = max((all + a.wide_wgs - 1) / a.wide_wgs, (long long)kLeastShare);
+  s.begin = index * s.length;
+  s.end = min(s.begin + s.length, all);
+  if (before <= s.begin && s.begin < before + sum) {  // (one thread, if the share is not empty)
+    sm_start[0] = tid * each;
+    sm_start[1] = before;
+  }
+  __syncthreads();
+  s.unit = 0;
+  s.at = s.end;
+  if (s.begin >= s.end) return s;
+  s.unit = of_lane(sm_start[0], 0);
+  s.at = of_lane(sm_start[1], 0);
+  while (each > 1) {
+    const long long cost = s.unit + lane < units ? window_unit(a, s.unit + lane).cost : 0;
+    long long upto = cost;
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) {
+      const long long up = __shfl_up(upto, sh);
+      if (lane >= sh) upto += up;
+    }
+    const unsigned long long behind = __builtin_amdgcn_ballot_w64(s.at + upto > s.begin);
+    if (behind) {
+      const int l = (int)__builtin_ctzll(behind);
+      s.unit += l;
+      s.at += of_lane(upto - cost, l);
+      return s;
+    }
+    s.unit += 64;
+    s.at += of_lane(upto, 63);
+  }
+  return s;
+}
+// The piece of a unit that share k has leaves its partials [column][ws_slot_floats(D)] in slot 2 k, or 2 k + 1 if it is the unit's first piece.
+template <int D>
+__device__ inline float *window_slot(const PagedChosenArgs &a, long long slot) {
+  return a.wide_slots + slot * kWideColumns * ws_slot_floats(D);
+}
+
+// kShares: a share of all units' tiles, else one unit.
+template <int D, bool kE4m3, bool kFp32, bool kShares>
 __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const PagedChosenArgs a, const long long first_wg) {
   constexpr int NG = 2, kWaveColumns = 16 * NG, kWaves = kWideThreads / 64, NK = D / 32, NB = D / 16;
   constexpr int kRow = 2 * D, kTileBytes = kChosenTile * kRow;
@@ -277,192 +375,255 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
   constexpr int NP = (2 * kChosenTile * kPieces + kWideThreads - 1) / kWideThreads;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int quad = lane >> 4, col = lane & 15;
-  const float c = a.scale_log2e;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[2][2 * kTileBytes];
   __shared__ int sm_bad[2][kWaves];
 
-  long long u = first_wg + blockIdx.x;
-  const int x = (int)(u % a.n_other);
-  u /= a.n_other;
-  const int part = (int)(u % a.parts_other);
-  u /= a.parts_other;
-  const int hx = a.n_past + x, h = a.head_of[hx];
-  int i, n;
-  const int b = tile_of(a, u, a.wide_tokens, i, n);
-  if (b < 0) return;
-  const int tokens = min(a.wide_tokens, n - i), live = tokens * a.g;
-  const long long token0 = (a.cu ? a.cu[b] : b) + i, w = (long long)b * a.Hkv + h;
-  int my_head[NG], my_from[NG], my_to[NG], my_token[NG];
-#pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    const int column = kWaveColumns * wave + 16 * g + col;
-    my_token[g] = column < live ? column / a.g : 0;
-    my_head[g] = column < live ? column - my_token[g] * a.g : 0;
-    token_window(a, w, hx, i + my_token[g], n, my_from[g], my_to[g]);
-  }
-  // first and last row that one token sees, and that every one sees
-  int from, first_to, last_from, to;
-  token_window(a, w, hx, i, n, from, first_to);
-  token_window(a, w, hx, i + tokens - 1, n, last_from, to);
-  from = __builtin_amdgcn_readfirstlane(from);
-  last_from = __builtin_amdgcn_readfirstlane(last_from);
-  first_to = __builtin_amdgcn_readfirstlane(first_to);
-  to = __builtin_amdgcn_readfirstlane(to);
-  const bool idle = kWaveColumns * wave >= live;  // a wave without columns only helps to load
-
-  const int *table = table_of(a.c, a.Hkv, b, h);
-  const int hh = a.c.per_head ? 0 : h;
   int koff[NK], voff[NB];
   operand_places<D>(kTileBytes, koff, voff);
-  WaveColumns<D, kFp32, NG> cols;
-  cols.clear();
-#pragma unroll
-  for (int g = 0; g < NG; ++g)
-    cols.load(g, a.q + ((token0 + my_token[g]) * a.Hq + h * a.g + my_head[g]) * D + 8 * quad, kWaveColumns * wave + 16 * g + col < live);
-
-  // ---- the halves' places, 64 at a time, a lane each (every wave for itself)
-  int half_row = -1;
-  long long half_at = 0, half_place = 0;
-  auto look_up = [&](int t) {
-    half_row = -1;
-    half_at = 0;
-    half_place = 0;
-    const long long r = 16ll * (2 * (t + (lane >> 1)) + (lane & 1)) + from / kChosenTile * kChosenTile;
-    if (r >= to || r + 16 <= from) return;
-    int in_page;
-    const int page = page_of(a.c, table, (int)r, in_page);
-    if (page < 0) return;
-    half_row = (int)r;
-    half_at = page * a.c.page_bytes + hh * a.c.head_bytes + in_page * a.c.row_bytes;
-    half_place = ((long long)page * a.c.heads + hh) * a.c.page_rows.d + in_page;
-  };
-
-  // A wave's pieces are all of keys or all of values, and of one half.
-  const unsigned char *const pool_k = a.c.k, *const pool_v = a.c.v, *const scale_k = a.c.k_scale, *const scale_v = a.c.v_scale;
-  struct Flight {  // a tile's pieces on their way
-    u32x4 x[NP];
-    int scale[NP];
-  } flight0, flight1;
-  auto piece_of = [&](int p, int &row, int &half) __attribute__((always_inline)) {
-    const int first = p * kWideThreads + 64 * wave;
-    row = (first + lane) / kPieces % kChosenTile;
-    half = first / (16 * kPieces) % 2;
-    return first >= kChosenTile * kPieces;
-  };
-  const bool loads = 64 * wave < 2 * kChosenTile * kPieces;
-  auto fetch = [&](Flight &f, int j) __attribute__((always_inline)) {
-    if (!loads) return;
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      int row, half;
-      const bool is_v = piece_of(p, row, half);
-      const unsigned char *src = (is_v ? pool_v : pool_k) + of_lane(half_at, 2 * j + half);
-      f.x[p] = *(const u32x4 *)(src + (unsigned)(row & 15) * (unsigned)a.c.row_bytes + lane % kPieces * 16);
-      if constexpr (kE4m3) f.scale[p] = (is_v ? scale_v : scale_k)[of_lane(half_place, 2 * j + half) + (row & 15)];
-    }
-  };
-  auto stage = [&](const Flight &f, int buf, unsigned valid, bool mixed) __attribute__((always_inline)) {
-    bool bad = false;
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      if (!loads) break;
-      int row, half;
-      const bool is_v = piece_of(p, row, half);
-      unsigned char *dst = tiles[buf] + (is_v ? kTileBytes : 0);
-      if (is_v && (mixed || valid != ~0u)) bad |= stage_piece<D, kE4m3>(dst, row, lane % kPieces, f.x[p], f.scale[p], true, !((valid >> row) & 1), mixed);
-      else stage_piece<D, kE4m3>(dst, row, lane % kPieces, f.x[p], f.scale[p], is_v, false, false);
-    }
-    if (mixed) {
-      const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
-      if (lane == 0) sm_bad[buf][wave] = any;
-    }
-  };
-
-  // ---- tiles t_begin .. t_end - 1, those without a row left out
-  const int all = to > 0 ? (to + kChosenTile - 1) / kChosenTile - from / kChosenTile : 0;
-  const int per_part = (all + a.parts_other - 1) / a.parts_other, t_begin = min(part * per_part, all), t_end = min(t_begin + per_part, all);
   int buf = 0;
-  for (int t = t_begin; t < t_end; t += 32) {
-    look_up(t);
-    unsigned long long halves = __builtin_amdgcn_ballot_w64(half_row >= 0);
-    if (t_end - t < 32) halves &= (1ull << (2 * (t_end - t))) - 1;
-    unsigned long long some = (halves | (halves >> 1)) & 0x5555555555555555ull;
-    if (!some) continue;
-    // One tile is computed, the next one waits in registers, and the one behind it is asked for: with one less in flight a tile took as
-    // long as its keys needed to come.
-    struct Tile {
-      int j, row0, row1;
-      unsigned valid;
-      bool mixed;  // some tokens see all of it, others do not
-    } tile0, tile1;
-    auto next_tile = [&]() __attribute__((always_inline)) {
-      Tile x;
-      x.j = some ? (int)__builtin_ctzll(some) >> 1 : -1;
-      some &= some - 1;
-      const int l = x.j < 0 ? 0 : 2 * x.j;
-      x.row0 = __builtin_amdgcn_readlane(half_row, l);
-      x.row1 = __builtin_amdgcn_readlane(half_row, l + 1);
-      x.valid = half_bits(x.row0, from, to) | half_bits(x.row1, from, to) << 16;
-      x.mixed = (x.row0 >= 0 && (x.row0 < last_from || x.row0 + 16 > first_to)) || (x.row1 >= 0 && (x.row1 < last_from || x.row1 + 16 > first_to));
-      return x;
-    };
-    auto step = [&](Tile &now, Flight &free, const Tile &then, const Flight &there) __attribute__((always_inline)) {
-      const Tile behind = next_tile();  // (none behind the last one)
-      if (behind.j >= 0) fetch(free, behind.j);
-      if (!idle) {
-        // (a half that is not there: rows behind the last one)
-        cols.tile(tiles[buf], koff, voff, c, now.mixed || now.valid != ~0u, now.row0 < 0 ? 0x7fffffc0 : now.row0, now.row1 < 0 ? 0x7fffffc0 : now.row1,
-                  my_from, my_to);
-        bool bad = false;
-        if (now.mixed)
-          for (int y = 0; y < kWaves; ++y) bad |= sm_bad[buf][y] != 0;
-        if (bad) {
+  // (workgroups are dealt out to the 8 XCDs in turn; neighbouring shares read the same rows and belong into one XCD's L2)
+  const float c = a.scale_log2e;
+  const long long wg = first_wg + blockIdx.x, index = wg % 8 * (a.wide_wgs / 8) + wg / 8;
+  WindowShare share;
+  if constexpr (kShares) {
+    share = window_share(a, index);
+  } else {
+    share.unit = wg % a.n_other * a.wide_tiles + wg / a.n_other;
+    share.at = 0;
+    share.end = 1;
+  }
+  if (kShares && tid == 0) a.splits[index].y = -1;
+  long long at = share.at;
 #pragma unroll 1
-          for (int r = 0; r < kChosenTile; ++r) {
-            if (!((now.valid >> r) & 1)) continue;
-            const int from_lane = 2 * now.j + (r >> 4);
-            float scale = 1.f;
-            if constexpr (kE4m3) scale = __uint_as_float((unsigned)scale_v[of_lane(half_place, from_lane) + (r & 15)] << 23);
-            cols.template odd_values<kE4m3>(pool_v + of_lane(half_at, from_lane) + (long long)(r & 15) * a.c.row_bytes, scale,
-                                            (r < 16 ? now.row0 : now.row1) + (r & 15), my_from, my_to);
+  for (long long u = share.unit; at < share.end; ++u) {
+    const WindowUnit unit = window_unit(a, u);
+    const int b = __builtin_amdgcn_readfirstlane(unit.b), i = __builtin_amdgcn_readfirstlane(unit.i), n = __builtin_amdgcn_readfirstlane(unit.n);
+    if (!kShares) at = 1;
+    if (b < 0) continue;
+    const int tokens = min(a.wide_tokens, n - i), live = tokens * a.g;
+    const int hx = a.n_past + __builtin_amdgcn_readfirstlane(unit.x), h = a.head_of[hx];
+    const long long token0 = (a.cu ? a.cu[b] : b) + i, w = (long long)b * a.Hkv + h;
+    int my_head[NG], my_from[NG], my_to[NG], my_token[NG];
+  #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int column = kWaveColumns * wave + 16 * g + col;
+      my_token[g] = column < live ? column / a.g : 0;
+      my_head[g] = column < live ? column - my_token[g] * a.g : 0;
+      token_window(a, w, hx, i + my_token[g], n, my_from[g], my_to[g]);
+    }
+    // first and last row that one token sees, and that every one sees
+    int from, first_to, last_from, to;
+    token_window(a, w, hx, i, n, from, first_to);
+    token_window(a, w, hx, i + tokens - 1, n, last_from, to);
+    from = __builtin_amdgcn_readfirstlane(from);
+    last_from = __builtin_amdgcn_readfirstlane(last_from);
+    first_to = __builtin_amdgcn_readfirstlane(first_to);
+    to = __builtin_amdgcn_readfirstlane(to);
+    const bool idle = kWaveColumns * wave >= live;  // a wave without columns only helps to load
+
+    const int *table = table_of(a.c, a.Hkv, b, h);
+    const int hh = a.c.per_head ? 0 : h;
+    WaveColumns<D, kFp32, NG> cols;
+    cols.clear();
+  #pragma unroll
+    for (int g = 0; g < NG; ++g)
+      cols.load(g, a.q + ((token0 + my_token[g]) * a.Hq + h * a.g + my_head[g]) * D + 8 * quad, kWaveColumns * wave + 16 * g + col < live);
+
+    // ---- the halves' places, 64 at a time, a lane each (every wave for itself)
+    int half_row = -1;
+    long long half_at = 0, half_place = 0;
+    auto look_up = [&](int t) {
+      half_row = -1;
+      half_at = 0;
+      half_place = 0;
+      const long long r = 16ll * (2 * (t + (lane >> 1)) + (lane & 1)) + from / kChosenTile * kChosenTile;
+      if (r >= to || r + 16 <= from) return;
+      int in_page;
+      const int page = page_of(a.c, table, (int)r, in_page);
+      if (page < 0) return;
+      half_row = (int)r;
+      half_at = page * a.c.page_bytes + hh * a.c.head_bytes + in_page * a.c.row_bytes;
+      half_place = ((long long)page * a.c.heads + hh) * a.c.page_rows.d + in_page;
+    };
+
+    // A wave's pieces are all of keys or all of values, and of one half.
+    const unsigned char *const pool_k = a.c.k, *const pool_v = a.c.v, *const scale_k = a.c.k_scale, *const scale_v = a.c.v_scale;
+    struct Flight {  // a tile's pieces on their way
+      u32x4 x[NP];
+      int scale[NP];
+    } flight0, flight1;
+    auto piece_of = [&](int p, int &row, int &half) __attribute__((always_inline)) {
+      const int first = p * kWideThreads + 64 * wave;
+      row = (first + lane) / kPieces % kChosenTile;
+      half = first / (16 * kPieces) % 2;
+      return first >= kChosenTile * kPieces;
+    };
+    const bool loads = 64 * wave < 2 * kChosenTile * kPieces;
+    auto fetch = [&](Flight &f, int j) __attribute__((always_inline)) {
+      if (!loads) return;
+  #pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        int row, half;
+        const bool is_v = piece_of(p, row, half);
+        const unsigned char *src = (is_v ? pool_v : pool_k) + of_lane(half_at, 2 * j + half);
+        f.x[p] = *(const u32x4 *)(src + (unsigned)(row & 15) * (unsigned)a.c.row_bytes + lane % kPieces * 16);
+        if constexpr (kE4m3) f.scale[p] = (is_v ? scale_v : scale_k)[of_lane(half_place, 2 * j + half) + (row & 15)];
+      }
+    };
+    auto stage = [&](const Flight &f, int buf, unsigned valid, bool mixed) __attribute__((always_inline)) {
+      bool bad = false;
+  #pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        if (!loads) break;
+        int row, half;
+        const bool is_v = piece_of(p, row, half);
+        unsigned char *dst = tiles[buf] + (is_v ? kTileBytes : 0);
+        if (is_v && (mixed || valid != ~0u)) bad |= stage_piece<D, kE4m3>(dst, row, lane % kPieces, f.x[p], f.scale[p], true, !((valid >> row) & 1), mixed);
+        else stage_piece<D, kE4m3>(dst, row, lane % kPieces, f.x[p], f.scale[p], is_v, false, false);
+      }
+      if (mixed) {
+        const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
+        if (lane == 0) sm_bad[buf][wave] = any;
+      }
+    };
+
+    // ---- tiles t_begin .. t_end - 1, those without a row left out
+    const int cost = __builtin_amdgcn_readfirstlane(unit.cost);
+    const int begin = kShares ? (int)max(share.begin - at, 0ll) : 0, end = kShares ? (int)min(share.end - at, (long long)cost) : cost;
+    const int t_begin = __builtin_amdgcn_readfirstlane(unit.tile_at(begin)), t_end = __builtin_amdgcn_readfirstlane(unit.tile_at(end));
+    const bool first_piece = begin == 0, whole = !kShares || (first_piece && end == cost);
+    if (kShares) {
+      // (of this unit the first piece, but not all: the last one too is for some share)
+      if (first_piece && !whole && tid == 0) a.splits[index] = int4{(int)u, (int)(u >> 32), (int)((at + cost - 1) / share.length), 0};
+      at += cost;
+    }
+    for (int t = t_begin; t < t_end; t += 32) {
+      look_up(t);
+      unsigned long long halves = __builtin_amdgcn_ballot_w64(half_row >= 0);
+      if (t_end - t < 32) halves &= (1ull << (2 * (t_end - t))) - 1;
+      unsigned long long some = (halves | (halves >> 1)) & 0x5555555555555555ull;
+      if (!some) continue;
+      // One tile is computed, the next one waits in registers, and the one behind it is asked for: with one less in flight a tile took as
+      // long as its keys needed to come.
+      struct Tile {
+        int j, row0, row1;
+        unsigned valid;
+        bool mixed;  // some tokens see all of it, others do not
+      } tile0, tile1;
+      auto next_tile = [&]() __attribute__((always_inline)) {
+        Tile x;
+        x.j = some ? (int)__builtin_ctzll(some) >> 1 : -1;
+        some &= some - 1;
+        const int l = x.j < 0 ? 0 : 2 * x.j;
+        x.row0 = __builtin_amdgcn_readlane(half_row, l);
+        x.row1 = __builtin_amdgcn_readlane(half_row, l + 1);
+        x.valid = half_bits(x.row0, from, to) | half_bits(x.row1, from, to) << 16;
+        x.mixed = (x.row0 >= 0 && (x.row0 < last_from || x.row0 + 16 > first_to)) || (x.row1 >= 0 && (x.row1 < last_from || x.row1 + 16 > first_to));
+        return x;
+      };
+      auto step = [&](Tile &now, Flight &free, const Tile &then, const Flight &there) __attribute__((always_inline)) {
+        const Tile behind = next_tile();  // (none behind the last one)
+        if (behind.j >= 0) fetch(free, behind.j);
+        if (!idle) {
+          // (a half that is not there: rows behind the last one)
+          cols.tile(tiles[buf], koff, voff, c, now.mixed || now.valid != ~0u, now.row0 < 0 ? 0x7fffffc0 : now.row0, now.row1 < 0 ? 0x7fffffc0 : now.row1,
+                    my_from, my_to);
+          bool bad = false;
+          if (now.mixed)
+            for (int y = 0; y < kWaves; ++y) bad |= sm_bad[buf][y] != 0;
+          if (bad) {
+  #pragma unroll 1
+            for (int r = 0; r < kChosenTile; ++r) {
+              if (!((now.valid >> r) & 1)) continue;
+              const int from_lane = 2 * now.j + (r >> 4);
+              float scale = 1.f;
+              if constexpr (kE4m3) scale = __uint_as_float((unsigned)scale_v[of_lane(half_place, from_lane) + (r & 15)] << 23);
+              cols.template odd_values<kE4m3>(pool_v + of_lane(half_at, from_lane) + (long long)(r & 15) * a.c.row_bytes, scale,
+                                              (r < 16 ? now.row0 : now.row1) + (r & 15), my_from, my_to);
+            }
           }
         }
-      }
-      buf ^= 1;
-      if (then.j < 0) return false;
-      stage(there, buf, then.valid, then.mixed);
+        buf ^= 1;
+        if (then.j < 0) return false;
+        stage(there, buf, then.valid, then.mixed);
+        __syncthreads();
+        now = behind;
+        return true;
+      };
+      tile0 = next_tile();
+      fetch(flight0, tile0.j);
+      tile1 = next_tile();
+      if (tile1.j >= 0) fetch(flight1, tile1.j);
+      stage(flight0, buf, tile0.valid, tile0.mixed);
       __syncthreads();
-      now = behind;
-      return true;
-    };
-    tile0 = next_tile();
-    fetch(flight0, tile0.j);
-    tile1 = next_tile();
-    if (tile1.j >= 0) fetch(flight1, tile1.j);
-    stage(flight0, buf, tile0.valid, tile0.mixed);
-    __syncthreads();
-    while (step(tile0, flight0, tile1, flight1) && step(tile1, flight1, tile0, flight0)) {
+      while (step(tile0, flight0, tile1, flight1) && step(tile1, flight1, tile0, flight0)) {
+      }
     }
-  }
 
-  // ---- results: a column's lanes hold four channels each
-  if (idle) return;
-#pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    const float l = over_quads(cols.l[g], true);
-    if (kWaveColumns * wave + 16 * g + col >= live) continue;
-    const long long token = token0 + my_token[g];
-    if (a.parts_other > 1) {
-      float *dst = partial_of<D>(a, false, token, x, part) + my_head[g] * ws_slot_floats(D);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(dst + 16 * nb + 4 * quad) = cols.O[g][nb];
-      if (quad == 0) *(float2 *)(dst + D) = float2{cols.m[g], l};
-    } else {
-      const float ref = cols.m[g] == -INFINITY ? 0.f : cols.m[g];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) store_out<D>(a, token * a.Hq + h * a.g + my_head[g], 16 * nb + 4 * quad, cols.O[g][nb], l, ref);
+    // ---- results: a column's lanes hold four channels each
+    if (idle) continue;
+  #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const float l = over_quads(cols.l[g], true);
+      const int column = kWaveColumns * wave + 16 * g + col;
+      if (column >= live) continue;
+      if (!whole) {
+        float *dst = window_slot<D>(a, 2ll * index + first_piece) + column * ws_slot_floats(D);
+  #pragma unroll
+        for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(dst + 16 * nb + 4 * quad) = cols.O[g][nb];
+        if (quad == 0) *(float2 *)(dst + D) = float2{cols.m[g], l};
+      } else {
+        const float ref = cols.m[g] == -INFINITY ? 0.f : cols.m[g];
+  #pragma unroll
+        for (int nb = 0; nb < NB; ++nb) store_out<D>(a, (token0 + my_token[g]) * a.Hq + h * a.g + my_head[g], 16 * nb + 4 * quad, cols.O[g][nb], l, ref);
+      }
     }
   }
+}
+
+// The units whose pieces are several workgroups': of the one whose first piece is workgroup k's, some columns.
+template <int D>
+__global__ __launch_bounds__(256) void paged_windows_join_kernel(const PagedChosenArgs a) {
+  constexpr int SF = D + kWsTailFloats, kLanes = D / 4, kEach = 256 / kLanes, kWgs = kWideColumns / kEach, kBatch = 4;
+  const int k = blockIdx.x / kWgs;
+  const int4 s = a.splits[k];
+  if (s.y < 0) return;
+  const WindowUnit unit = window_unit(a, ((long long)s.y << 32) | (unsigned)s.x);
+  const int column = blockIdx.x % kWgs * kEach + threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
+  if (column >= unit.tokens * a.g) return;
+  const int pieces = s.z - k + 1;
+  float top = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < pieces; p0 += kBatch) {
+    float2 ml[kBatch];
+    f32x4 y[kBatch];
+#pragma unroll
+    for (int p = 0; p < kBatch; ++p) {
+      const int piece = min(p0 + p, pieces - 1);
+      const float *src = window_slot<D>(a, 2ll * (k + piece) + (piece == 0)) + column * SF;
+      ml[p] = *(const float2 *)(src + D);
+      y[p] = *(const f32x4 *)(src + d);
+      if (p0 + p >= pieces) ml[p] = float2{-INFINITY, 0.f};
+    }
+    float m_new = top;
+#pragma unroll
+    for (int p = 0; p < kBatch; ++p) m_new = fmaxf(m_new, ml[p].x);
+    const float ref = m_new == -INFINITY ? 0.f : m_new, keep = __builtin_amdgcn_exp2f(top - ref);
+    l *= keep;
+    o *= keep;
+    top = m_new;
+#pragma unroll
+    for (int p = 0; p < kBatch; ++p) {
+      if (p0 + p < pieces) {
+        const float wgt = __builtin_amdgcn_exp2f(ml[p].x - ref);
+        l += ml[p].y * wgt;
+        o += y[p] * wgt;
+      }
+    }
+  }
+  const int token = column / a.g, hx = a.n_past + unit.x;
+  const long long first = (a.cu ? a.cu[unit.b] : unit.b) + unit.i;
+  store_out<D>(a, (first + token) * a.Hq + a.head_of[hx] * a.g + column - token * a.g, d, o, l, top == -INFINITY ? 0.f : top);
 }
 
 // ---- listed blocks ------------------------------------------------------------------------------
@@ -629,10 +790,14 @@ __global__ __launch_bounds__(256) void paged_listed_join_kernel(const PagedChose
 
 template <int D, bool kE4m3>
 static hipError_t launch_windows(const PagedChosenArgs &a, hipStream_t st) {
-  const auto kern = a.out_fp32 ? paged_windows_kernel<D, kE4m3, true> : paged_windows_kernel<D, kE4m3, false>;
-  return launch_in_parts(a.wgs_other, kWideThreads, [&](long long first, unsigned count) {
+  const auto kern = a.wide_wgs > 0 ? (a.out_fp32 ? paged_windows_kernel<D, kE4m3, true, true> : paged_windows_kernel<D, kE4m3, false, true>)
+                                   : (a.out_fp32 ? paged_windows_kernel<D, kE4m3, true, false> : paged_windows_kernel<D, kE4m3, false, false>);
+  const hipError_t e = launch_in_parts(a.wide_wgs > 0 ? a.wide_wgs : a.wgs_other, kWideThreads, [&](long long first, unsigned count) {
     hipLaunchKernelGGL(kern, dim3(count), dim3(kWideThreads), 0, st, a, first);
   });
+  if (e != hipSuccess || a.wide_wgs == 0) return e;
+  hipLaunchKernelGGL(paged_windows_join_kernel<D>, dim3(a.wide_wgs * (kWideColumns * D / 1024)), dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 hipError_t launch_paged_windows(const PagedChosenArgs &a, hipStream_t st) {
   return a.D == 128 ? (a.c.e4m3 ? launch_windows<128, true>(a, st) : launch_windows<128, false>(a, st))

@@ -75,6 +75,10 @@ struct PagedChosenArgs {
   // Many tokens at a time: tiles of windows, and listed blocks turned round, a part of the tokens after the other.
   int wide_windows, by_block;
   int wide_tokens;      // tokens whose heads are the columns of a window's workgroup
+  long long wide_tiles; // of that many tokens, in all sequences (some are empty)
+  int wide_wgs;         // workgroups that the windows' tiles are shared out to, a multiple of 8; 0: a workgroup for each of wide_tokens tokens
+  int4 *splits;         // of each of them: the unit whose first piece is its (two words, -1: none), the workgroup of the last piece
+  float *wide_slots;    // partials of pieces, two of kWideColumns columns for each
   int listed_tokens;    // most tokens of a task
   int listed_pieces;    // of a block, kListedRows rows each
   int blocks;           // of a window
@@ -99,6 +103,8 @@ struct PagedChosenArgs {
 };
 constexpr int kChosenTile = 32;
 constexpr int kWideColumns = 128;  // of a window's workgroup
+constexpr int kUnitTiles = 2;      // what a window's workgroup takes to begin and to end, in tiles
+constexpr int kLeastShare = 4;     // tiles
 constexpr int kListedRows = 64;
 // Shares the windows out (parts, tiles, workgroups) and lays the workspace out from `ws` on; returns its bytes.
 unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, unsigned char *ws);

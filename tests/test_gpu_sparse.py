@@ -492,6 +492,23 @@ def test_attention_of_ragged_tokens_in_bf16(kind):
     _attend(pool, blocks.rows, [150, 2, 64], 4, hq=12, policy=[1, 2, 3], seg=100, tail=7, out_fp32=False)
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d,g", [(128, 4), (64, 16)])
+def test_attention_of_windows_shared_by_many_workgroups(d, g, e4m3):
+    """Windows long enough to be cut into many pieces, one with the start of a segment amid the tokens of a piece, one after which nothing is left."""
+    new, held = [17, 40, 0, 1], [1990, 3500, 100, 0]
+    pool, blocks = _pool(dict(page_rows=64, block=64, e4m3=e4m3), [h + n for h, n in zip(held, new)], d=d, hkv=3)
+    _attend(pool, blocks.rows, new, 4, hq=3 * g, policy=[1, 2, 0], seg=1000, tail=300, total=sum(new) + 2)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_attention_of_windows_of_many_short_sequences(e4m3):
+    """So many that each (sequence, head) has a workgroup of its own: more than 2048."""
+    new = [(1, 2, 0, 5)[i % 4] for i in range(700)]
+    pool, blocks = _pool(dict(page_rows=16, block=16, e4m3=e4m3), [n + i % 31 for i, n in enumerate(new)], hkv=3)
+    _attend(pool, blocks.rows, new, 2, hq=12, policy=[1, 0, 1], seg=16, tail=4)
+
+
 def test_attention_of_lists_in_parts_of_the_tokens():
     """More partials than the workspace holds at a time: the tokens go in parts, to the same results as in calls of their own."""
     pool, _ = _pool(dict(page_rows=256, block=64), [9000], hkv=1)
