@@ -339,7 +339,7 @@ __device__ inline WindowShare window_share(const PagedChosenArgs &a, long long i
   if (s.begin >= s.end) return s;
   s.unit = of_lane(sm_start[0], 0);
   s.at = of_lane(sm_start[1], 0);
-  while (each > 1) {
+  while (each > 1 && s.unit < units) {
     const long long cost = s.unit + lane < units ? window_unit(a, s.unit + lane).cost : 0;
     long long upto = cost;
 #pragma unroll
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
   if (kShares && tid == 0) a.splits[index].y = -1;
   long long at = share.at;
 #pragma unroll 1
-  for (long long u = share.unit; at < share.end; ++u) {
+  for (long long u = share.unit; at < share.end && u < a.wgs_other; ++u) {
     const WindowUnit unit = window_unit(a, u);
     const int b = __builtin_amdgcn_readfirstlane(unit.b), i = __builtin_amdgcn_readfirstlane(unit.i), n = __builtin_amdgcn_readfirstlane(unit.n);
     if (!kShares) at = 1;
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
     const int hx = a.n_past + __builtin_amdgcn_readfirstlane(unit.x), h = a.head_of[hx];
     const long long token0 = (a.cu ? a.cu[b] : b) + i, w = (long long)b * a.Hkv + h;
     int my_head[NG], my_from[NG], my_to[NG], my_token[NG];
-  #pragma unroll
+#pragma unroll
     for (int g = 0; g < NG; ++g) {
       const int column = kWaveColumns * wave + 16 * g + col;
       my_token[g] = column < live ? column / a.g : 0;
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
     const int hh = a.c.per_head ? 0 : h;
     WaveColumns<D, kFp32, NG> cols;
     cols.clear();
-  #pragma unroll
+#pragma unroll
     for (int g = 0; g < NG; ++g)
       cols.load(g, a.q + ((token0 + my_token[g]) * a.Hq + h * a.g + my_head[g]) * D + 8 * quad, kWaveColumns * wave + 16 * g + col < live);
 
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
     const bool loads = 64 * wave < 2 * kChosenTile * kPieces;
     auto fetch = [&](Flight &f, int j) __attribute__((always_inline)) {
       if (!loads) return;
-  #pragma unroll
+#pragma unroll
       for (int p = 0; p < NP; ++p) {
         int row, half;
         const bool is_v = piece_of(p, row, half);
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
     };
     auto stage = [&](const Flight &f, int buf, unsigned valid, bool mixed) __attribute__((always_inline)) {
       bool bad = false;
-  #pragma unroll
+#pragma unroll
       for (int p = 0; p < NP; ++p) {
         if (!loads) break;
         int row, half;
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
           if (now.mixed)
             for (int y = 0; y < kWaves; ++y) bad |= sm_bad[buf][y] != 0;
           if (bad) {
-  #pragma unroll 1
+#pragma unroll 1
             for (int r = 0; r < kChosenTile; ++r) {
               if (!((now.valid >> r) & 1)) continue;
               const int from_lane = 2 * now.j + (r >> 4);
@@ -562,19 +562,19 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
 
     // ---- results: a column's lanes hold four channels each
     if (idle) continue;
-  #pragma unroll
+#pragma unroll
     for (int g = 0; g < NG; ++g) {
       const float l = over_quads(cols.l[g], true);
       const int column = kWaveColumns * wave + 16 * g + col;
       if (column >= live) continue;
       if (!whole) {
         float *dst = window_slot<D>(a, 2ll * index + first_piece) + column * ws_slot_floats(D);
-  #pragma unroll
+#pragma unroll
         for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(dst + 16 * nb + 4 * quad) = cols.O[g][nb];
         if (quad == 0) *(float2 *)(dst + D) = float2{cols.m[g], l};
       } else {
         const float ref = cols.m[g] == -INFINITY ? 0.f : cols.m[g];
-  #pragma unroll
+#pragma unroll
         for (int nb = 0; nb < NB; ++nb) store_out<D>(a, (token0 + my_token[g]) * a.Hq + h * a.g + my_head[g], 16 * nb + 4 * quad, cols.O[g][nb], l, ref);
       }
     }
