@@ -227,7 +227,7 @@ __device__ inline unsigned order_key(int dot, int scale) {
 // and then the largest over a token's heads.  GP: heads of a token in a tile, a power of two up to 16; a group of more takes passes
 // of 16.
 constexpr int kScoreSets = 4;
-template <int D, int GP>
+template <int D>
 struct QueryRows {
   static constexpr int NK = D / 64;
   i32x4 up[NK], down[NK];  // this lane's 16 channels of every 64, of row lane % 16: what is above zero, and what is below
@@ -261,18 +261,15 @@ __device__ __attribute__((always_inline)) void score_blocks(const PagedChooseArg
   const int lane = threadIdx.x & 63, quad = lane >> 4, col = lane & 15;
   const int *table = table_of(a.k.c, a.k.Hkv, b, h);
   const int passes = GP < 16 ? 1 : (a.g + 15) / 16;
-  QueryRows<D, GP> rows[QT];
-  const unsigned short *q0[QT];
   const int head = col % GP;  // of this lane's query row
-#pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
+  // A set's queries (of head 0), and the scale of every token's.
+  auto queries = [&](int qt, int &shift) __attribute__((always_inline)) {
     const int token = qt * (16 / GP) + col / GP;
-    q0[qt] = a.q + ((t + (token < here ? token : 0)) * a.Hq + h * a.g) * D + 16 * quad;
-    // the largest magnitude of every token's queries
-    float most = 0.f;
+    const unsigned short *q0 = a.q + ((t + (token < here ? token : 0)) * a.Hq + h * a.g) * D + 16 * quad;
+    float most = 0.f;  // the largest magnitude
     for (int p = 0; p < passes; ++p) {
       if (p * 16 + head < a.g) {
-        const unsigned short *q = q0[qt] + (p * 16 + head) * D;
+        const unsigned short *q = q0 + (p * 16 + head) * D;
 #pragma unroll
         for (int kc = 0; kc < NK; ++kc)
 #pragma unroll
@@ -288,12 +285,37 @@ __device__ __attribute__((always_inline)) void score_blocks(const PagedChooseArg
     for (int sh = 1; sh < GP; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
-    rows[qt].shift = most > 0.f ? -scale_exponent(most) : 0;
-  }
+    shift = most > 0.f ? -scale_exponent(most) : 0;
+    return q0;
+  };
+  QueryRows<D> rows[QT];
+  const unsigned short *q0 = nullptr;
   // (rows beyond the group repeat the pass's head 0, which the largest value does not notice)
-  auto take = [&](int qt, int p) __attribute__((always_inline)) { rows[qt].round(q0[qt] + (p * 16 + (p * 16 + head < a.g ? head : 0)) * D); };
+  auto take = [&](int p) __attribute__((always_inline)) { rows[0].round(q0 + (p * 16 + (p * 16 + head < a.g ? head : 0)) * D); };
+  if constexpr (QT > 1) {  // each of the workgroup's four waves rounds a set (all of them by every wave: 2533 tokens 79 us instead of 63)
+    static_assert(QT == 4, "");
+    __shared__ i32x4 sm_rows[QT][2 * NK][64];
+    const int mine = threadIdx.x >> 6;
+    q0 = queries(mine, rows[0].shift);
+    take(0);
+    __syncthreads();  // (the tokens before are read)
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) take(qt, 0);
+    for (int kc = 0; kc < NK; ++kc) {
+      sm_rows[mine][kc][lane] = rows[0].up[kc];
+      sm_rows[mine][NK + kc][lane] = rows[0].down[kc];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+      for (int kc = 0; kc < NK; ++kc) {
+        rows[qt].up[kc] = sm_rows[qt][kc][lane];
+        rows[qt].down[kc] = sm_rows[qt][NK + kc][lane];
+      }
+  } else {
+    q0 = queries(0, rows[0].shift);
+    take(0);
+  }
   const int step = 16 * kAtOnce * waves;
   for (int j0 = a.first + 16 * kAtOnce * wave; j0 < hi; j0 += step) {
     i32x4 bd[kAtOnce][2 * NK];
@@ -316,7 +338,7 @@ __device__ __attribute__((always_inline)) void score_blocks(const PagedChooseArg
       for (int qt = 0; qt < QT; ++qt) {
         int best[4];
         for (int p = 0; p < passes; ++p) {
-          if (passes > 1) take(qt, p);
+          if (passes > 1) take(p);
           i32x4 S = {0, 0, 0, 0};
 #pragma unroll
           for (int kc = 0; kc < NK; ++kc) {
@@ -528,9 +550,9 @@ __device__ __attribute__((always_inline)) void pick_blocks(const Keys keys, int 
 
 // Scores and choice in one launch: a tile's keys stay in LDS.  A token's picks are found by one wave where the tile has several tokens, by
 // all waves together where it has one.
-template <int D, int GP, int kThreads>
-__global__ __launch_bounds__(kThreads) void paged_choose_kernel(const PagedChooseArgs a, const long long first_wg) {
-  constexpr int kWaves = kThreads / 64;
+template <int D, int GP>
+__global__ __launch_bounds__(256) void paged_choose_kernel(const PagedChooseArgs a, const long long first_wg) {
+  constexpr int kThreads = 256, kWaves = kThreads / 64;
   extern __shared__ unsigned sm_keys[];  // [token of the tile][stride]
   __shared__ union {
     Team<kWaves> all;
@@ -584,14 +606,15 @@ static hipError_t launch_choose(const PagedChooseArgs &a, hipStream_t st) {
   if (a.in_lds) {
     const size_t lds = (size_t)a.tile * a.stride * 4;
     return launch_in_parts((a.total + a.tile - 1) / a.tile * a.k.n_past, 256, [&](long long first, unsigned count) {
-      hipLaunchKernelGGL((paged_choose_kernel<D, GP, 256>), dim3(count), dim3(256), lds, st, a, first);
+      hipLaunchKernelGGL((paged_choose_kernel<D, GP>), dim3(count), dim3(256), lds, st, a, first);
     });
   }
   for (long long t = 0; t < a.total; t += a.part) {
     const long long n = a.total - t < a.part ? a.total - t : a.part, units = n * a.k.n_past, tiles = (n + a.tile - 1) / a.tile * a.k.n_past;
-    // enough workgroups to fill the card, none with fewer than 128 blocks
+    // enough workgroups to fill the card, none with fewer than 128 blocks (3 a compute unit and 6: 64 sequences of up to 64K rows, eight heads,
+    // 28.7 us and 30.4 with the choice; 2533 tokens of four heads 63 and 65)
     const long long groups = (a.stride + 127) / 128;
-    long long share = (6 * device_cus() + tiles - 1) / tiles;
+    long long share = (3 * device_cus() + tiles - 1) / tiles;
     share = share < 1 ? 1 : share > groups ? groups : share;
     PagedChooseArgs part = a;
     part.total = t + n;
