@@ -47,8 +47,8 @@ __device__ inline s16x2 from_lane(s16x2 x, int mask) { return __builtin_bit_cast
 // A wave per block.  Lane l has 16 bytes, kChannels channels, of the rows l / kLanes, l / kLanes + kRows, ...  The largest and smallest keys
 // are found as bf16 (8-bit keys times their scales are), two at a time as whole numbers; a block in which one is not finite, or of scales
 // so small that bf16 would not hold the keys, is done again in 32 bits.  The lanes of a column then share its channels out.  Bound by memory
-// and by the chain row counts -> page -> rows.  (Runs of blocks for a wave, the next one's rows on their way: 147K 8-bit rows 56 us, one
-// block each 41.)
+// and by the chain row counts -> page -> rows: 152K 8-bit rows of eight heads 39.5 us, 4.1 TB/s (32 us where the last call left them in the caches);
+// with keys compared one by one in 32 bits 48, with runs of blocks for a wave, the next one's rows on their way, 56 instead of the 41 of then.
 // kAhead: loads of rows on their way.
 template <int D, bool kE4m3, int kAhead>
 __global__ __launch_bounds__(256) void paged_summarize_kernel(const PagedBlocksArgs a, const long long first_wg) {
@@ -388,7 +388,10 @@ __device__ inline bool tile_tokens(const PagedChooseArgs &a, long long t, long l
   return true;
 }
 
-// Keys to the workspace, where they do not fit LDS.
+// Keys to the workspace, where they do not fit LDS.  One token each: bound by memory behind the chain row counts -> page -> bounds (64 sequences
+// of up to 64K rows, eight heads, 72 MB of bounds: 23 us, 3.1 TB/s).  Many tokens: QT sets of 16 query rows meet each group of bounds in registers
+// (2533 tokens of four heads behind up to 60K rows 43 us, 0.39 POP/s; a set at a time 107), and what bounds it is the work on the sums -- the
+// largest of a token's heads, the order's key, a store each -- which is a few times that of the products.
 template <int D, int GP, int QT>
 __global__ __launch_bounds__(256) void paged_score_kernel(const PagedChooseArgs a, const long long t_first, const long long first_wg, const int wgs_per_unit) {
   const long long wg = first_wg + blockIdx.x, unit = wg / wgs_per_unit, tile = unit / a.k.n_past;
@@ -582,7 +585,8 @@ __global__ __launch_bounds__(256) void paged_choose_kernel(const PagedChooseArgs
   }
 }
 
-// The choice from keys in the workspace: a workgroup per (token, PAST head), or (kAlone) a wave.
+// The choice from keys in the workspace: a workgroup per (token, PAST head), or (kAlone) a wave.  Bound by the latencies of its two or three
+// rounds of counting: 10132 lists of 32 from up to 970 keys 23 us, 512 lists from up to 1024 keys 7.
 template <int kThreads, bool kAlone>
 __global__ __launch_bounds__(kThreads) void paged_select_kernel(const PagedChooseArgs a, const long long t_first, const long long units, const long long first_wg) {
   constexpr int kTeams = kAlone ? kThreads / 64 : 1, kWaves = kThreads / 64 / kTeams;

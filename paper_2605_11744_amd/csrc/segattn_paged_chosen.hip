@@ -5,7 +5,11 @@
 //   S^T[key][column] = K . Q^T            v_mfma_f32_16x16x32_bf16, A = K rows, B = Q^T (registers)
 //   P = exp2((S^T - m) c)                 running maximum m and sum l per column, in fp32
 //   O^T[d][column] += V^T . P^T           A = V^T via ds_read_b64_tr_b16, B = P from the S^T registers
-// P enters as two bf16 (what that leaves is below 2^-16 of a weight), for fp32 outputs as three.
+// P enters as two bf16 (what that leaves is below 2^-16 of a weight), for fp32 outputs as three: the matrix pipes idle beside the memory.
+// K and V go from memory to LDS through registers, a tile ahead, because the halves lie anywhere and 8-bit rows become bf16 on the way.  Bound by
+// memory where the workgroups fill the card (48 sequences of 8-bit rows, two heads with 32 blocks of 64 and six with windows up to 5K rows:
+// 58 us, 4.7 TB/s; without the windows' unequal lengths 6.3 to 6.7), else by the latency of a round of tiles, 1.2 us, and 9 us
+// around them (one sequence's 64 blocks: 9 us and 4 to join).
 #include <math.h>
 
 #include <type_traits>

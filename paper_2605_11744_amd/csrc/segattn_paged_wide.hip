@@ -6,6 +6,10 @@
 // list one block, whose rows are read once for all of them; a token's lists are turned round first (count, place, sort), each
 // (token, entry) leaves a partial (acc[D], m, l) per query head, and a last launch joins a token's partials.  Which
 // token lands in which column depends on the order of atomics, but no column's numbers depend on its neighbours.
+//
+// A chunk of 2533 tokens behind up to 60K rows, eight KV heads of four query heads, half of them long-range with 32 blocks of 64 rows: windows 194 us
+// and 16 to join (73 GFLOP, 375 TFLOP/s: eight waves a compute unit do not hide a tile's chain of scores, maximum, exponentials and products),
+// listed blocks 221 (0.68 GB of partials written, 3.1 TB/s), their join 118 (read, 5.7 TB/s), turning the lists round 41.
 #include "segattn_paged_chosen.h"
 
 namespace segattn {

@@ -339,6 +339,16 @@ def test_choose_among_many_blocks_and_up_to_max_rows():
     _choose(pool, blocks, [2], 40, 3, 4, hq=2, max_rows=33333)
 
 
+@pytest.mark.parametrize("g", [1, 2, 3, 5, 8])
+@pytest.mark.parametrize("d", [64, 128])
+def test_choose_for_chunks_behind_many_blocks(d, g):
+    """Tokens that share the bounds they are scored with, in tiles that end amid sequences and hold several."""
+    new = [70, 3, 0, 130, 5, 1]
+    pool, blocks = _pool(dict(page_rows=64, block=16), [5000, 5200, 4000, 900, 4777, 4200], d=d, hkv=2)
+    _random_bounds(pool, blocks)
+    _choose(pool, blocks, new, 24, 1, 2, hq=2 * g, policy=[2, 3], total=sum(new) + 3)
+
+
 def test_choose_in_parts_of_the_tokens():
     """More keys than the workspace holds at a time: the tokens go in parts."""
     pool, blocks = _pool(dict(page_rows=16, block=16), [3000], hkv=1, d=64)
