@@ -367,6 +367,18 @@ bool blocks_one_by_one(const PagedChosenArgs &a, double parts, double tiles) {
   return 30 + (2 * partials + (listed < all ? listed : all)) / 5e6 < (rounds > bytes ? rounds : bytes);
 }
 
+// Whether the windows of several tokens a sequence share their tiles, by how long both ways take (us, with the longest window's tiles): 128 columns
+// cost what they cost however few of them are tokens', but single tokens read the rows anew, from the caches if that.  Measured, alone and
+// shared, in us, windows up to 5K rows: a 130K history, eight heads, 4 tokens 16 and 31, 16 tokens 27 and 37, 32 tokens 40 and 40, 64 tokens 60 and
+// 43; 48 sequences of 8-bit rows, six heads of eight, 2 tokens 113 and 164, 3 tokens 157 and 172, 4 tokens 200 and 175 (bf16 rows: 186
+// and 184, 270 and 206 for three); eight of them, 4 tokens 45 and 57, 8 tokens 68 and 62.
+bool windows_share_tiles(const PagedChosenArgs &a, double tiles) {
+  const double bytes = 2.0 * a.D * (a.c.e4m3 ? 1 : 2), row = bytes / 512, alone = (double)a.total * a.n_other * tiles;
+  const double shared = (double)a.n_other * (a.cu ? (double)a.total / a.wide_tokens + a.B : (double)a.total) * tiles;
+  const double cached = (double)a.B * a.n_other * tiles * kChosenTile * bytes <= 40e6 ? 0.6 : 1;
+  return 10 + alone * cached * (0.5 + 0.9 * row) * 1e-3 > 38 + shared * (1.8 + row) * 1e-3;
+}
+
 unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, unsigned char *ws) {
   unsigned long long at = 0;
   const auto take = [&](auto *&x, unsigned long long count) {
@@ -377,17 +389,17 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
   const bool many = max_seqlen > 1 && a.g <= kColumns;
   a.wide_tokens = many ? kWideColumns / a.g : 1;
   a.listed_tokens = kListedColumns / a.g > 0 ? kListedColumns / a.g : 1;
-  a.wide_windows = many && a.n_other > 0;
-  a.wide_tiles = a.cu ? a.total / a.wide_tokens + a.B : a.total;
   const int block_rows = 16 * (int)a.block_halves.d;
   a.blocks = (int)(((long long)a.max_rows + block_rows - 1) / block_rows);
   a.listed_pieces = (block_rows + kListedRows - 1) / kListedRows;
   long long units_past = a.total * a.n_past * a.passes;
-  const long long units_other = a.n_other * (a.wide_windows ? a.wide_tiles : a.total * a.passes);
   const long long halves = (long long)a.n_chosen * a.block_halves.d;
   long long window = (long long)a.seg.d + a.tail + a.wide_tokens;
   window = window < a.max_rows ? window : a.max_rows;
   const long long tiles_past = a.n_past ? (halves + 1) / 2 : 1, tiles_other = window / kChosenTile + 2;
+  a.wide_windows = many && a.n_other > 0 && windows_share_tiles(a, tiles_other);
+  a.wide_tiles = a.cu ? a.total / a.wide_tokens + a.B : a.total;
+  const long long units_other = a.n_other * (a.wide_windows ? a.wide_tiles : a.total * a.passes);
   const long long units = units_past + (a.wide_windows ? 0 : units_other);
   // Windows are shared out while there are fewer workgroups than two per compute unit of a 256-CU part.
   auto share = [&](long long tiles, long long p, long long least, int &parts, int &per_part) {

@@ -502,21 +502,44 @@ def test_attention_of_ragged_tokens_in_bf16(kind):
     _attend(pool, blocks.rows, [150, 2, 64], 4, hq=12, policy=[1, 2, 3], seg=100, tail=7, out_fp32=False)
 
 
-@pytest.mark.parametrize("e4m3", [False, True])
-@pytest.mark.parametrize("d,g", [(128, 4), (64, 16)])
-def test_attention_of_windows_shared_by_many_workgroups(d, g, e4m3):
-    """Windows long enough to be cut into many pieces, one with the start of a segment amid the tokens of a piece, one after which nothing is left."""
-    new, held = [17, 40, 0, 1], [1990, 3500, 100, 0]
-    pool, blocks = _pool(dict(page_rows=64, block=64, e4m3=e4m3), [h + n for h, n in zip(held, new)], d=d, hkv=3)
-    _attend(pool, blocks.rows, new, 4, hq=3 * g, policy=[1, 2, 0], seg=1000, tail=300, total=sum(new) + 2)
+# Tokens so many that their windows share tiles, in windows long enough to be cut into many pieces: the start of a segment amid the tokens of a piece,
+# sequences without tokens, with one and without a row before.
+SHARED = [(dict(page_rows=64, block=64), 128, 4, True), (dict(page_rows=128, block=64, per_head=True, e4m3=True), 128, 4, False),
+          (dict(page_rows=48, block=48, token_major=True), 64, 4, True), (dict(page_rows=80, block=80, e4m3=True), 64, 1, True),
+          (dict(page_rows=64, block=64), 128, 16, False), (dict(page_rows=32, block=16, per_head=True), 128, 3, True)]
+
+
+@pytest.mark.parametrize("kind,d,g,out_fp32", SHARED, ids=range(len(SHARED)))
+def test_attention_of_windows_that_share_tiles(kind, d, g, out_fp32):
+    new, held = [900, 1100, 0, 1], [1990, 3500, 100, 0]
+    pool, blocks = _pool(kind, [h + n for h, n in zip(held, new)], d=d, hkv=3)
+    _attend(pool, blocks.rows, new, 4, hq=3 * g, policy=[1, 2, 0], seg=1000, tail=300, total=sum(new) + 2, out_fp32=out_fp32)
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
-def test_attention_of_windows_of_many_short_sequences(e4m3):
-    """So many that each (sequence, head) has a workgroup of its own: more than 2048."""
-    new = [(1, 2, 0, 5)[i % 4] for i in range(700)]
-    pool, blocks = _pool(dict(page_rows=16, block=16, e4m3=e4m3), [n + i % 31 for i, n in enumerate(new)], hkv=3)
-    _attend(pool, blocks.rows, new, 2, hq=12, policy=[1, 0, 1], seg=16, tail=4)
+def test_windows_that_share_tiles_are_not_touched_by_rows_that_are_not_seen(e4m3):
+    """NaN before every window and before some, behind tokens' own rows, at a segment's start, in a row without a page; infinities in one channel."""
+    for odd_row in ((100, 690, 1000, 2100, 2800, 3499), (1990, 2999)):
+        pool, _ = _pool(dict(page_rows=32, block=32, e4m3=e4m3), [3500], hkv=3)
+        for r in odd_row:
+            for h in range(3):
+                page, hh, i = pool.place(0, h, [r])
+                for x in (pool.k, pool.v) if len(odd_row) > 2 else (pool.v,):
+                    if e4m3 or len(odd_row) > 2:
+                        x[page.cuda(), hh, i.cuda()] = 0x7F if e4m3 else math.nan
+                    else:
+                        x[page.cuda(), hh, i.cuda(), 7] = math.inf if r == 2999 else -math.inf
+        pool.table[0, 1600 // 32] = -1
+        out, lse, odd = _attend(pool, 32, [2000], 3, hq=12, policy=[1, 2, 0], seg=1000, tail=300)
+        assert not odd.all() and odd.any() and out[~odd].isfinite().all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_attention_of_windows_with_a_workgroup_each(e4m3):
+    """So many tokens and heads that windows are not cut: 2064 times eight tokens in one head's window."""
+    new, held = [2044, 6], [130, 0]
+    pool, blocks = _pool(dict(page_rows=64, block=64, e4m3=e4m3), [h + n for h, n in zip(held, new)], hkv=8)
+    _attend(pool, blocks.rows, new, 1, hq=128, policy=[1, 0, 1, 1, 0, 0, 1, 1], seg=200, tail=56, out_fp32=not e4m3)
 
 
 def test_attention_of_lists_in_parts_of_the_tokens():
