@@ -184,9 +184,11 @@ struct WaveColumns {
         for (int r = 0; r < 4; ++r) S[g][h2][r] *= c;
       float mx = fmaxf(fmaxf(fmaxf(S[g][0][0], S[g][0][1]), fmaxf(S[g][0][2], S[g][0][3])), fmaxf(fmaxf(S[g][1][0], S[g][1][1]), fmaxf(S[g][1][2], S[g][1][3])));
       mx = over_quads(mx, false);
-      if (__builtin_amdgcn_ballot_w64(mx - m[g] > kLag)) {  // (also where a first row is seen: infinite)
-        const float m_new = fmaxf(m[g], mx), alpha = __builtin_amdgcn_exp2f(m[g] - (m_new == -INFINITY ? 0.f : m_new));
-        m[g] = m_new;
+      // (also where a first row is seen: infinite.  Column by column: which one lies beside it must not show in a column's roundings)
+      const bool grows = mx - m[g] > kLag;
+      if (__builtin_amdgcn_ballot_w64(grows)) {
+        const float alpha = grows ? __builtin_amdgcn_exp2f(m[g] - mx) : 1.f;
+        m[g] = grows ? mx : m[g];
         l[g] *= alpha;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) O[g][nb] *= alpha;
