@@ -19,6 +19,11 @@ __device__ inline int scale_exponent(float most) {
   const float m = frexpf(most, &x);
   return x - 7 + (m > 127.f / 128.f ? 1 : 0);
 }
+// x / 2^e rounded up, for quotients of at most 127: one above zero is 1 or more, also where it is below the smallest float.
+__device__ inline int rounded_up(float x, int e) {
+  const int y = (int)ceilf(ldexpf(x, -e));
+  return x > 0.f && y < 1 ? 1 : y;
+}
 __device__ inline float finite_or_zero(float x) { return fabsf(x) < INFINITY ? x : 0.f; }
 
 // Where block j of a window has its bounds and its scale (and the first of its rows): -1 without a page.
@@ -192,8 +197,8 @@ __global__ __launch_bounds__(256) void paged_summarize_kernel(const PagedBlocksA
   int exponent = most > 0.f ? scale_exponent(most) : kLeastBoundExponent;
   exponent = exponent < kLeastBoundExponent ? kLeastBoundExponent : exponent;
   if (!writes) return;
-  const int up0 = (int)ceilf(ldexpf(top[0], -exponent)), up1 = (int)ceilf(ldexpf(top[1], -exponent));
-  const int down0 = (int)floorf(ldexpf(bottom[0], -exponent)), down1 = (int)floorf(ldexpf(bottom[1], -exponent));
+  const int up0 = rounded_up(top[0], exponent), up1 = rounded_up(top[1], exponent);
+  const int down0 = -rounded_up(-bottom[0], exponent), down1 = -rounded_up(-bottom[1], exponent);
   signed char *dst = a.bounds + at.block * (2 * D) + kChannels * col + 2 * pair;
   *(unsigned short *)dst = (unsigned short)((up0 & 255) | (up1 & 255) << 8);
   *(unsigned short *)(dst + D) = (unsigned short)((down0 & 255) | (down1 & 255) << 8);
