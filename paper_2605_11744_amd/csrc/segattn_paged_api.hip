@@ -195,6 +195,14 @@ bool shared_bytes(const Bytes (&outs)[kOuts], const Bytes (&ins)[kIns]) {
 unsigned long long table_entries(const Problem &p, const PagedCache &c) {
   return (unsigned long long)p.B * (c.per_head ? p.Hkv : 1) * c.max_pages;
 }
+// One of the outputs shares bytes with the table or with an array of the pool that holds a value per row.
+template <size_t kOuts>
+bool shared_with_pool(const Bytes (&outs)[kOuts], const Problem &p, const PagedCache &c) {
+  const unsigned long long rows = (unsigned long long)c.n_pages * c.heads * c.page_rows.d;
+  const Bytes pool[] = {{c.table, 4 * table_entries(p, c)}, {c.e4m3 ? c.k_scale : nullptr, rows}, {c.e4m3 ? c.v_scale : nullptr, rows},
+                        {c.mass, 4 * rows}, {c.pos, 4 * rows}};
+  return shared_bytes(outs, pool);
+}
 
 // A packed batch of new tokens; one without any is a batch too.
 bool batch_size_fits(const Problem &p, int64_t total, int64_t max_seqlen) {
@@ -551,8 +559,8 @@ segattn_status seg_kv_paged_summarize(const segattn_config *cfg, const segattn_p
   if (p.n_past == 0 || !rows || max_new < 1 || max_new >= kMostRows) return SEGATTN_EINVAL;
   if (misaligned(rows_from, 4) || misaligned(rows, 4) || foreign(stream)) return SEGATTN_EINVAL;
   const Bytes outs[] = {bounds_bytes(a), scale_bytes(a)};
-  const Bytes ins[] = {{rows, 4ull * p.B * p.Hkv}, {rows_from, 4ull * p.B * p.Hkv}, {pages->table, 4 * table_entries(p, c)}};
-  if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+  const Bytes ins[] = {{rows, 4ull * p.B * p.Hkv}, {rows_from, 4ull * p.B * p.Hkv}};
+  if (shared_bytes(outs, ins) || shared_with_pool(outs, p, c)) return SEGATTN_EINVAL;
   a.rows_from = rows_from;
   a.rows = rows;
   a.most = (int)((max_new + blocks->block_rows - 1) / blocks->block_rows);
@@ -588,8 +596,8 @@ segattn_status seg_kv_paged_choose(const segattn_config *cfg, const segattn_page
   if (misaligned(q, 16) || misaligned(rows, 4) || misaligned(chosen, 4) || misaligned(workspace, kAlign) || foreign(stream)) return SEGATTN_EINVAL;
   const Bytes outs[] = {{chosen, 4ull * total * p.n_past * n_chosen}, {workspace, bytes}};
   const Bytes ins[] = {{q, 2ull * total * p.Hq * p.D}, {rows, 4ull * p.B * p.Hkv}, {cu_seqlens, 4ull * (p.B + 1ull)},
-                       {pages->table, 4 * table_entries(p, c)}, bounds_bytes(a.k), scale_bytes(a.k)};
-  if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+                       bounds_bytes(a.k), scale_bytes(a.k)};
+  if (shared_bytes(outs, ins) || shared_with_pool(outs, p, c)) return SEGATTN_EINVAL;
   if (total == 0) return SEGATTN_OK;
   a.q = (const unsigned short *)q;
   a.cu = cu_seqlens;
@@ -640,8 +648,8 @@ segattn_status seg_attn_paged_chosen(const segattn_config *cfg, const segattn_pa
   const unsigned long long heads = (unsigned long long)total * p.Hq;
   const Bytes outs[] = {{out, heads * p.D * (p.out_fp32 ? 4 : 2)}, {lse, heads * 4}, {workspace, bytes}};
   const Bytes ins[] = {{q, heads * p.D * 2}, {rows, 4ull * p.B * p.Hkv}, {cu_seqlens, 4ull * (p.B + 1ull)},
-                       {p.n_past ? chosen : nullptr, 4ull * total * p.n_past * n_chosen}, {pages->table, 4 * table_entries(p, c)}};
-  if (shared_bytes(outs, ins)) return SEGATTN_EINVAL;
+                       {p.n_past ? chosen : nullptr, 4ull * total * p.n_past * n_chosen}};
+  if (shared_bytes(outs, ins) || shared_with_pool(outs, p, c)) return SEGATTN_EINVAL;
   if (total == 0) return SEGATTN_OK;
   a.q = (const unsigned short *)q;
   a.rows = rows;
