@@ -227,6 +227,17 @@ bool reserve_space(const Problem &p, const PagedCache &c, ReserveSpace &s) {
   return true;
 }
 
+// Whether one workgroup does it all.  A thread of it goes through a sequence's entries one after the other, 0.25 us for each and head that wants
+// it (tables per head: 0.6), and looks at them twice.  Measured, one workgroup and four launches, in us, eight heads: 256 sequences with an entry
+// each 13 and 19 (tables per head 19 and 21), 8 with 4 entries 15 and 18 (25 and 18), 4 with 5 16 and 16, 2 with 6 19 and 16, one with 21
+// 50 and 16 (100 and 17); one head, 2560 entries, 1454 and 22.
+bool reserve_by_one_workgroup(const Problem &p, const PagedCache &c, int64_t total, int64_t max_seqlen) {
+  // a row range of m rows meets (m + page_rows - 2) / page_rows + 1 entries at most
+  const long long entries = (max_seqlen + c.page_rows.d - 2) / c.page_rows.d + 1;
+  return p.B <= 256 && c.n_pages <= (1 << 18) && total * p.Hkv <= 2560 && (long long)p.B * p.Hkv * entries <= kSmallReserve &&
+         p.Hkv * entries <= (c.per_head ? 10 : 40);
+}
+
 void fill_tables(const Problem &p, const segattn_pages *pages, PagedTablesArgs &a) {
   fill_heads(p, a.heads);
   a.table = const_cast<int32_t *>(pages->table);  // (the caller's device memory; the two calls that write it say so)
@@ -527,9 +538,7 @@ segattn_status seg_kv_paged_reserve(const segattn_config *cfg, const segattn_pag
   a.chunks = (int)s.chunks;
   a.heads_div = fast_div_by(p.Hkv);
   a.longest = (int)max_seqlen;
-  // a row range of m rows meets (m + page_rows - 2) / page_rows + 1 entries at most
-  const long long entries = (max_seqlen + a.c.page_rows.d - 2) / a.c.page_rows.d + 1;
-  a.small = p.B <= 256 && a.c.n_pages <= (1 << 18) && total * p.Hkv <= 2560 && (long long)p.B * p.Hkv * entries <= kSmallReserve;
+  a.small = reserve_by_one_workgroup(p, a.c, total, max_seqlen);
   return hip_status(launch_paged_reserve(a, (hipStream_t)stream));
 }
 

@@ -1,5 +1,7 @@
-// The form that a call of seg_attn_paged_chosen takes, from the library's own rules (linked from libsegattn.so).  One call per
-// input line, one answer per output line:
+// The form that a call of seg_attn_paged_chosen or seg_kv_paged_reserve takes, from the library's own rules (linked from libsegattn.so).  One
+// call per input line, one answer per output line:
+//   reserve heads sequences page_rows n_pages per_head total longest
+//       -> "one" (workgroup) | "four" (launches)
 //   D Hq Hkv policy S T batch total longest max_rows block_rows n_chosen e4m3 out_fp32
 //       -> listed blocks: "blocks" (a block once for the tokens that list it) | "tokens"; tokens of a part;
 //          windows: "shares" (cut evenly) | "units" (a workgroup each) | "tokens"; workgroups of the windows;
@@ -11,6 +13,20 @@
 #include <vector>
 
 #include "segattn_paged_api.hip"  // build_paged, build_pages, chosen_space
+
+static bool reserve(const std::string &line) {
+  std::istringstream in(line);
+  std::string word;
+  long long total, longest;
+  int page_rows;
+  Problem p;
+  PagedCache c;
+  in >> word >> p.Hkv >> p.B >> page_rows >> c.n_pages >> c.per_head >> total >> longest;
+  if (in.fail() || !batch_size_fits(p, total, longest)) return false;
+  c.page_rows = fast_div_by(page_rows);
+  std::cout << (reserve_by_one_workgroup(p, c, total, longest) ? "one" : "four") << '\n';
+  return true;
+}
 
 static bool answer(const std::string &line) {
   std::istringstream in(line);
@@ -51,7 +67,7 @@ static bool answer(const std::string &line) {
 
 int main() {
   for (std::string line; std::getline(std::cin, line);)
-    if (!answer(line)) {
+    if (!(line.rfind("reserve ", 0) == 0 ? reserve(line) : answer(line))) {
       std::cout << "refused: " << line << '\n';
       return 1;
     }

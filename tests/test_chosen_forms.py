@@ -1,4 +1,4 @@
-"""The form that attention over chosen blocks takes, asked from the library's rules on the CPU (tests/host/chosen_forms.hip): that the GPU tests
+"""The form that attention over chosen blocks and the reservation of pages take, asked from the library's rules on the CPU (tests/host/chosen_forms.hip): that the GPU tests
 written for a form have shapes that take it."""
 import os
 import shutil
@@ -27,7 +27,7 @@ def forms(tmp_path_factory):
         assert out.returncode == 0, out.stdout + out.stderr
         got = [x.split() for x in out.stdout.splitlines()]
         assert len(got) == len(lines)
-        return [dict(listed=x[0], part=int(x[1]), windows=x[2], workgroups=int(x[3]), laid_out=int(x[4]), asked=int(x[5])) for x in got]
+        return [x[0] if len(x) == 1 else dict(listed=x[0], part=int(x[1]), windows=x[2], workgroups=int(x[3]), laid_out=int(x[4]), asked=int(x[5])) for x in got]
 
     return ask
 
@@ -42,3 +42,12 @@ def test_chunks_whose_columns_are_compared_share_blocks_and_tiles(forms):
     got = forms([line(d=d, g=g, policy=POLICY, seg=SEG, tail=TAIL, new=[n], most=-(-(HELD + n) // BLOCK) * BLOCK, block=BLOCK, chosen=chosen, e4m3=e4m3, out_fp32=f)
                  for d, g, e4m3, n, chosen in CHUNKS for f in (True, False)])
     assert [(x["listed"], x["windows"]) for x in got] == [("blocks", "shares")] * len(got)
+
+
+def test_a_thread_does_not_go_through_many_entries(forms):
+    """Few sequences with many entries each: one workgroup, a thread a sequence, takes up to a millisecond where four launches take 20 us."""
+    ask = lambda heads, sequences, page_rows, per_head, new: forms([f"reserve {heads} {sequences} {page_rows} 9000 {per_head} {sequences * new} {new}"])[0]
+    for many in ((1, 1, 1, 0, 2560), (8, 1, 16, 0, 320), (8, 1, 16, 1, 320), (8, 1, 1, 1, 320), (2, 1, 16, 0, 1280), (8, 8, 16, 1, 40)):
+        assert ask(*many) == "four", many
+    for step in ((8, 48, 64, 0, 1), (8, 256, 16, 1, 1), (8, 64, 64, 0, 5), (8, 8, 16, 0, 40), (2, 100, 16, 1, 1)):
+        assert ask(*step) == "one", step
