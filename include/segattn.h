@@ -581,7 +581,8 @@ segattn_status seg_kv_paged_summarize(const segattn_config *cfg, const segattn_p
  *     2^(scale_j - 127) * max over the group of sum over channels of q8 * (q8 > 0 ? upper_j : lower_j),
  * formed and compared exactly for scales as seg_kv_paged_summarize writes them: an upper bound of the block's largest score but for the
  * rounding of q.  A block without a page has the lowest score.
- * workspace: device, >= ..._workspace_bytes() (0: invalid arguments), 256-byte aligned, overwritten: calls that may overlap need one each. */
+ * workspace: device, >= ..._workspace_bytes() (0: invalid arguments), 256-byte aligned, overwritten: calls that may overlap need one each.  It
+ * has 4 bytes for each token, PAST head and block of max_rows, but no more than 256 MiB or (where that is more) 16 tokens': more go in parts. */
 size_t seg_kv_paged_choose_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
                                            const segattn_blocks *blocks, int64_t total, int64_t max_rows,
                                            int32_t n_chosen);
@@ -598,7 +599,9 @@ segattn_status seg_kv_paged_choose(const segattn_config *cfg, const segattn_page
  * [total,Hq]; rows without a page are not seen, and a query head that sees no row has zeros and -infinity; one that
  * sees a row of K or V with infinities or NaN may have NaN where the formula has an infinity, others are not touched by it.  Of
  * blocks only block_rows is looked at.  chosen may be NULL where no head has the PAST bit (n_chosen is then not looked at).
- * workspace as above. */
+ * workspace as above: up to 2.25 GiB.  Of that 1 GiB is for chunks of which a listed block is taken once for all tokens that list it (more
+ * tokens than it holds go in parts), 8 bytes for each block of their histories that max_rows leaves room for (1 GiB at most, beyond which
+ * lists are taken token by token), 70 MB for windows. */
 size_t seg_attn_paged_chosen_workspace_bytes(const segattn_config *cfg, const segattn_pages *pages,
                                              const segattn_blocks *blocks, int64_t total, int64_t max_seqlen,
                                              int64_t max_rows, int32_t n_chosen);

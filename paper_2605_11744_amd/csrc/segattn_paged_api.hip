@@ -276,7 +276,9 @@ bool choose_space(const Problem &p, const PagedBlocksArgs &k, int64_t total, int
   unsigned long long part = kChoiceSpace / per_token;
   part = part < 16 ? 16 : part;
   a.part = (int)(part < (unsigned long long)total ? part : total);
-  bytes = align_up(a.part * per_token);
+  // (not of whole tokens, so that a call's bytes cover those of fewer tokens or rows)
+  const unsigned long long all = (unsigned long long)total * per_token, most = kChoiceSpace > 16 * per_token ? kChoiceSpace : 16 * per_token;
+  bytes = align_up(all < most ? all : most);
   bytes = bytes ? bytes : kAlign;
   return true;
 }
@@ -310,7 +312,10 @@ bool chosen_space(const Problem &p, const PagedCache &c, const segattn_blocks *b
     a.head_of[i] = (unsigned char)p.order[i];
     a.tail_of[i] = (p.policy[p.order[i]] & SEGATTN_TAIL) != 0;
   }
-  bytes = total == 0 ? 0 : align_up(plan_paged_chosen(a, max_seqlen, (unsigned char *)ws));
+  bytes = kAlign;
+  if (total == 0) return true;
+  const unsigned long long planned = plan_paged_chosen(a, max_seqlen, (unsigned char *)ws), most = most_paged_chosen(a, max_seqlen);
+  bytes = align_up(most > planned ? most : planned);  // (never less than what is laid out)
   bytes = bytes ? bytes : kAlign;
   return true;
 }
@@ -629,14 +634,12 @@ size_t seg_attn_paged_chosen_workspace_bytes(const segattn_config *cfg, const se
   Problem p;
   PagedCache c;
   PagedChosenArgs a;
-  unsigned long long without, with;
+  unsigned long long bytes;
   memset(&a, 0, sizeof(a));
   if (!build_paged(cfg, p) || !build_pages(pages, p, c)) return 0;
   if (!batch_size_fits(p, total, max_seqlen)) return 0;
-  // (the call may come with cu_seqlens or, for one token of every sequence, without)
-  if (!chosen_space(p, c, blocks, nullptr, total, max_seqlen, max_rows, n_chosen, nullptr, a, without)) return 0;
-  if (!chosen_space(p, c, blocks, (const int32_t *)4, total, max_seqlen, max_rows, n_chosen, nullptr, a, with)) return 0;
-  return (size_t)(without > with ? without : with);
+  // (without cu_seqlens a sequence has one token, and then nothing depends on them)
+  return chosen_space(p, c, blocks, (const int32_t *)4, total, max_seqlen, max_rows, n_chosen, nullptr, a, bytes) ? (size_t)bytes : 0;
 }
 
 segattn_status seg_attn_paged_chosen(const segattn_config *cfg, const segattn_pages *pages, const segattn_blocks *blocks, const void *q,

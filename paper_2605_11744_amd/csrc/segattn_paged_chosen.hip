@@ -347,9 +347,16 @@ __global__ __launch_bounds__(256) void paged_chosen_join_kernel(const PagedChose
   }
 }
 
-constexpr long long kListedSpace = 1ull << 30;  // partials of listed blocks, of a token at least
+constexpr long long kListedSpace = 1ll << 30;  // bytes of partials of listed blocks at a time
+constexpr long long kMostKeys = 1ll << 27;     // (sequence, PAST head, block): two words for each
 constexpr long long kResident = 512;  // workgroups: two per compute unit of a 256-CU part
 constexpr int kListedColumns = 384;
+
+constexpr double kListedLaunches = 30;  // us
+double row_bytes(const PagedChosenArgs &a) { return 2.0 * a.D * (a.c.e4m3 ? 1 : 2); }  // keys and values
+
+// Bytes of partials that an entry of a list leaves.
+long long entry_bytes(const PagedChosenArgs &a) { return (long long)a.listed_pieces * a.g * (a.D + 2) * 4; }
 
 // Whether listed blocks are turned round and taken one by one, by how long both ways take (us).  Token by token: rounds of resident workgroups,
 // 32 rows of a wave at a time as they come from memory, or what all rows together need of the caches.  Block by block: the launches before and
@@ -358,14 +365,19 @@ constexpr int kListedColumns = 384;
 // tokens 222 and 137; heads of 64: 59 and 61, 176 and 94; one query head each: 64 tokens 66 and 64, 400 tokens 377 and 92); of an 8K history, 64
 // tokens 39 and 47, 128 tokens 73 and 65; two KV heads of eight query heads, 128 tokens 38 and 56, 400 tokens 114 and 84.
 bool blocks_one_by_one(const PagedChosenArgs &a, double parts, double tiles) {
-  const double row = 2.0 * a.D * (a.c.e4m3 ? 1 : 2), block = 16.0 * a.block_halves.d * row;
+  const double row = row_bytes(a), block = 16.0 * a.block_halves.d * row;
   const double entries = (double)a.total * a.n_past * a.n_chosen, listed = entries * block, all = (double)a.B * a.n_past * a.blocks * block;
   const double units = (double)a.total * a.n_past * a.passes * parts;
   const double rounds = ceil(units / kResident) * ceil(tiles / kChosenWaves) * 3.2 * row / 512;
   const double bytes = listed / (all <= 40e6 ? 14.5e6 : 8.5e6);
-  const double partials = entries * a.listed_pieces * a.g * (a.D + 2) * 4;
-  return 30 + (2 * partials + (listed < all ? listed : all)) / 5e6 < (rounds > bytes ? rounds : bytes);
+  const double partials = entries * entry_bytes(a);
+  return kListedLaunches + (2 * partials + (listed < all ? listed : all)) / 5e6 < (rounds > bytes ? rounds : bytes);
 }
+
+// Of the windows: launches, in us, and a tile of a token, or of a unit, in us.
+constexpr double kAloneLaunches = 10, kSharedLaunches = 38;
+double alone_tile(const PagedChosenArgs &a) { return (0.5 + 0.9 * row_bytes(a) / 512) * 1e-3; }
+double shared_tile(const PagedChosenArgs &a) { return (1.8 + row_bytes(a) / 512) * 1e-3; }
 
 // Whether the windows of several tokens a sequence share their tiles, by how long both ways take (us, with the longest window's tiles): 128 columns
 // cost what they cost however few of them are tokens', but single tokens read the rows anew, from the caches if that.  Measured, alone and
@@ -373,89 +385,137 @@ bool blocks_one_by_one(const PagedChosenArgs &a, double parts, double tiles) {
 // 43; 48 sequences of 8-bit rows, six heads of eight, 2 tokens 113 and 164, 3 tokens 157 and 172, 4 tokens 200 and 175 (bf16 rows: 186
 // and 184, 270 and 206 for three); eight of them, 4 tokens 45 and 57, 8 tokens 68 and 62.
 bool windows_share_tiles(const PagedChosenArgs &a, double tiles) {
-  const double bytes = 2.0 * a.D * (a.c.e4m3 ? 1 : 2), row = bytes / 512, alone = (double)a.total * a.n_other * tiles;
+  const double bytes = row_bytes(a), alone = (double)a.total * a.n_other * tiles;
   const double shared = (double)a.n_other * (a.cu ? (double)a.total / a.wide_tokens + a.B : (double)a.total) * tiles;
   const double cached = (double)a.B * a.n_other * tiles * kChosenTile * bytes <= 40e6 ? 0.6 : 1;
-  return 10 + alone * cached * (0.5 + 0.9 * row) * 1e-3 > 38 + shared * (1.8 + row) * 1e-3;
+  return kAloneLaunches + alone * cached * alone_tile(a) > kSharedLaunches + shared * shared_tile(a);
 }
 
-unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, unsigned char *ws) {
+// What a plan needs of the workspace.
+struct ChosenSpace {
+  unsigned long long partials = 0;  // of (token, head)s whose rows are shared out, g query heads each
+  unsigned long long shares = 0;    // of windows
+  unsigned long long keys = 0, entries = 0;
+};
+unsigned long long lay_out(PagedChosenArgs &a, const ChosenSpace &s, unsigned char *ws) {
   unsigned long long at = 0;
   const auto take = [&](auto *&x, unsigned long long count) {
     x = reinterpret_cast<std::remove_reference_t<decltype(x)>>(ws + at);
     at += (count * sizeof(*x) + 255) / 256 * 256;
   };
+  take(a.slots, s.partials * a.g * ws_slot_floats(a.D));
+  take(a.splits, s.shares);
+  take(a.wide_slots, 2 * s.shares * kWideColumns * ws_slot_floats(a.D));
+  if (s.entries == 0) return at;
+  take(a.cursors, s.keys + 2);
+  a.counts = a.cursors + 2;
+  take(a.offsets, s.keys);
+  take(a.rank, s.entries);
+  take(a.sorted, s.entries);
+  take(a.tasks, s.entries / a.listed_tokens + (s.entries < s.keys ? s.entries : s.keys));
+  take(a.listed_out, s.entries * a.listed_pieces * a.g * a.D);
+  take(a.listed_sum, s.entries * a.listed_pieces * a.g);
+  return at;
+}
+
+// Key tiles of a list, and of the longest window.
+struct ChosenTiles {
+  long long past, other;
+};
+ChosenTiles count_tiles(const PagedChosenArgs &a) {
+  const long long halves = (long long)a.n_chosen * a.block_halves.d;
+  long long window = (long long)a.seg.d + a.tail + a.wide_tokens;
+  window = window < a.max_rows ? window : a.max_rows;
+  return {a.n_past ? (halves + 1) / 2 : 1, window / kChosenTile + 2};
+}
+bool many_tokens(const PagedChosenArgs &a, long long max_seqlen) { return max_seqlen > 1 && a.g <= kColumns; }
+constexpr long long kLeastPart = 2 * kChosenWaves;  // tiles
+// Windows' workgroups that are resident (D = 64: three on a compute unit).
+long long windows_resident(const PagedChosenArgs &a) { return a.D == 128 ? kResident : kResident * 3 / 2; }
+// Shares that as many units can be cut into.
+long long most_shares(long long units, long long tiles, long long resident) {
+  if (units >= resident) return resident;
+  const long long most = units * (2 * tiles + kUnitTiles) / kLeastShare + 1;
+  return most < resident ? (most + 7) / 8 * 8 : resident;
+}
+
+unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, unsigned char *ws) {
+  ChosenSpace space;
   a.passes = (a.g + kColumns - 1) / kColumns;
-  const bool many = max_seqlen > 1 && a.g <= kColumns;
+  const bool many = many_tokens(a, max_seqlen);
   a.wide_tokens = many ? kWideColumns / a.g : 1;
   a.listed_tokens = kListedColumns / a.g > 0 ? kListedColumns / a.g : 1;
   const int block_rows = 16 * (int)a.block_halves.d;
   a.blocks = (int)(((long long)a.max_rows + block_rows - 1) / block_rows);
   a.listed_pieces = (block_rows + kListedRows - 1) / kListedRows;
   long long units_past = a.total * a.n_past * a.passes;
-  const long long halves = (long long)a.n_chosen * a.block_halves.d;
-  long long window = (long long)a.seg.d + a.tail + a.wide_tokens;
-  window = window < a.max_rows ? window : a.max_rows;
-  const long long tiles_past = a.n_past ? (halves + 1) / 2 : 1, tiles_other = window / kChosenTile + 2;
-  a.wide_windows = many && a.n_other > 0 && windows_share_tiles(a, tiles_other);
+  const ChosenTiles tiles = count_tiles(a);
+  a.wide_windows = many && a.n_other > 0 && windows_share_tiles(a, tiles.other);
   a.wide_tiles = a.cu ? a.total / a.wide_tokens + a.B : a.total;
   const long long units_other = a.n_other * (a.wide_windows ? a.wide_tiles : a.total * a.passes);
   const long long units = units_past + (a.wide_windows ? 0 : units_other);
   // Windows are shared out while there are fewer workgroups than two per compute unit of a 256-CU part.
-  auto share = [&](long long tiles, long long p, long long least, int &parts, int &per_part) {
-    const long long most = tiles / least;
+  auto share = [&](long long tiles, long long p, int &parts, int &per_part) {
+    const long long most = tiles / kLeastPart;
     p = p < most ? p : most;
     p = p < 1 ? 1 : p;
     per_part = (int)((tiles + p - 1) / p);
     parts = (int)((tiles + per_part - 1) / per_part);
   };
   const long long narrow = units >= kResident || units == 0 ? 1 : kResident / units;
-  share(tiles_past, narrow, 2 * kChosenWaves, a.parts_past, a.tiles_past);
-  const double keys = (double)a.B * a.n_past * a.blocks;
-  a.by_block = many && a.n_past > 0 && keys < 1e9 && (double)a.n_past * a.n_chosen * a.listed_pieces < 1e8 && blocks_one_by_one(a, a.parts_past, a.tiles_past);
+  share(tiles.past, narrow, a.parts_past, a.tiles_past);
+  const long long keys = (long long)a.B * a.n_past * a.blocks, per_token = (long long)a.n_past * a.n_chosen, at_once = kListedSpace / entry_bytes(a);
+  a.by_block = many && a.n_past > 0 && keys <= kMostKeys && per_token <= at_once && blocks_one_by_one(a, a.parts_past, a.tiles_past);
   // (windows are of all lengths up to the longest: twice as many, so that it is not waited for: 48 sequences of 8-bit rows 65 us with a workgroup each
   // and 60 with four, 30 of them 44 and 43, eight 20 and 23)
   const long long ragged = units >= kResident || units == 0 ? 1 : (kResident * 2 + units - 1) / units;
-  share(tiles_other, a.wide_windows ? 1 : ragged, 2 * kChosenWaves, a.parts_other, a.tiles_other);
+  share(tiles.other, a.wide_windows ? 1 : ragged, a.parts_other, a.tiles_other);
   if (a.by_block) {
     a.parts_past = 1;
     units_past = 0;
   }
   a.wgs_past = units_past * a.parts_past;
   a.wgs_other = units_other * a.parts_other;
-  unsigned long long slots = 0;
-  if (a.parts_past > 1) slots += (unsigned long long)a.total * a.n_past * a.parts_past;
-  if (a.parts_other > 1) slots += (unsigned long long)a.total * a.n_other * a.parts_other;
-  take(a.slots, slots * a.g * ws_slot_floats(a.D));
+  if (a.parts_past > 1) space.partials += (unsigned long long)a.total * a.n_past * a.parts_past;
+  if (a.parts_other > 1) space.partials += (unsigned long long)a.total * a.n_other * a.parts_other;
   if (a.wide_windows) {
-    // Shares of equal length for as many workgroups as are resident (D = 64: three on a compute unit), but where the units alone are several
-    // rounds of them, a workgroup for each (8 heads with windows up to 5K, new tokens: 2048 342 us in shares and 449 by units,
-    // 8192 1041 and 1039, 16384 2105 and 2018).
-    const long long resident = a.D == 128 ? kResident : kResident * 3 / 2;
-    a.wide_wgs = 0;
-    if (units_other < 4 * resident) {
-      const long long most = units_other * (2 * tiles_other + kUnitTiles) / kLeastShare + 1;
-      a.wide_wgs = (int)(most < resident ? (most + 7) / 8 * 8 : resident);
-    }
-    take(a.splits, a.wide_wgs);
-    take(a.wide_slots, 2ll * a.wide_wgs * kWideColumns * ws_slot_floats(a.D));
+    // Shares of equal length for as many workgroups as are resident, but where the units alone are several rounds of them, a workgroup for
+    // each (8 heads with windows up to 5K, new tokens: 2048 342 us in shares and 449 by units, 8192 1041 and 1039, 16384 2105 and 2018).
+    const long long resident = windows_resident(a);
+    a.wide_wgs = units_other < 4 * resident ? (int)most_shares(units_other, tiles.other, resident) : 0;
+    space.shares = a.wide_wgs;
   }
   if (a.by_block) {
-    const long long per_token = (long long)a.n_past * a.n_chosen;  // < 2^23
-    long long part = kListedSpace / (per_token * a.listed_pieces * a.g * (a.D + 2) * 4);
-    part = part < 1 ? 1 : part < a.total ? part : a.total;
-    a.part_tokens = (int)part;
-    const unsigned long long n_keys = (unsigned long long)keys, entries = part * per_token;
-    take(a.cursors, n_keys + 2);
-    a.counts = a.cursors + 2;
-    take(a.offsets, n_keys);
-    take(a.rank, entries);
-    take(a.sorted, entries);
-    take(a.tasks, entries / a.listed_tokens + (entries < n_keys ? entries : n_keys));
-    take(a.listed_out, entries * a.listed_pieces * a.g * a.D);
-    take(a.listed_sum, entries * a.listed_pieces * a.g);
+    const long long part = at_once / per_token;
+    a.part_tokens = (int)(part < a.total ? part : a.total);
+    space.keys = keys;
+    space.entries = a.part_tokens * per_token;
   }
-  return at;
+  return lay_out(a, space, ws);
+}
+
+// Room for this call and every smaller one: with fewer tokens (in all, of a sequence), sequences, rows or listed blocks, which may take other
+// forms.  So a form counts where what it saves, without what it costs, lets any of them take it; what it then needs grows with the sizes.
+unsigned long long most_paged_chosen(PagedChosenArgs a, long long max_seqlen) {
+  const bool many = many_tokens(a, max_seqlen);
+  const ChosenTiles tiles = count_tiles(a);
+  ChosenSpace space;
+  // Rows are shared out while there are fewer than kResident units of the passes: lists in kResident / units parts, windows in 2 kResident / units,
+  // rounded up, so that all parts together are fewer than 3 kResident.
+  const auto parts = [](long long tiles) { return tiles / kLeastPart > 1 ? tiles / kLeastPart : 0; };
+  const long long cut = a.total * (a.n_past * parts(tiles.past) + a.n_other * parts(tiles.other)), most_cut = 3 * kResident / a.passes + 1;
+  space.partials = cut < most_cut ? cut : most_cut;
+  const double alone = (double)a.total * a.n_other * tiles.other;
+  if (many && a.n_other > 0 && kAloneLaunches + alone * (alone_tile(a) - shared_tile(a) / a.wide_tokens) > kSharedLaunches)
+    space.shares = most_shares(a.n_other * (a.total / a.wide_tokens + a.B), tiles.other, windows_resident(a));
+  const double rounds = ceil((double)a.total * a.n_past * a.passes / kResident) * ceil((double)tiles.past / kChosenWaves) * 3.2 * row_bytes(a) / 512;
+  const double listed = (double)a.total * a.n_past * a.n_chosen * 16.0 * a.block_halves.d * row_bytes(a) / 8.5e6;
+  if (many && a.n_past > 0 && kListedLaunches < (rounds > listed ? rounds : listed)) {
+    const long long keys = (long long)a.B * a.n_past * a.blocks, entries = a.total * a.n_past * a.n_chosen, at_once = kListedSpace / entry_bytes(a);
+    space.keys = keys < kMostKeys ? keys : kMostKeys;
+    space.entries = entries < at_once ? entries : at_once;
+  }
+  return lay_out(a, space, nullptr);
 }
 
 template <int D>

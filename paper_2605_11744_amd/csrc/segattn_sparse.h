@@ -108,6 +108,8 @@ constexpr int kLeastShare = 4;     // tiles
 constexpr int kListedRows = 64;
 // Shares the windows out (parts, tiles, workgroups) and lays the workspace out from `ws` on; returns its bytes.
 unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, unsigned char *ws);
+// Bytes that no plan of these sizes, or of smaller ones, exceeds (of a planned call's arguments).
+unsigned long long most_paged_chosen(PagedChosenArgs a, long long max_seqlen);
 hipError_t launch_paged_windows(const PagedChosenArgs &a, hipStream_t st);
 hipError_t launch_paged_listed(const PagedChosenArgs &a, hipStream_t st);
 hipError_t launch_paged_chosen(const PagedChosenArgs &a, hipStream_t st);

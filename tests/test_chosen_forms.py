@@ -51,3 +51,53 @@ def test_a_thread_does_not_go_through_many_entries(forms):
         assert ask(*many) == "four", many
     for step in ((8, 48, 64, 0, 1), (8, 256, 16, 1, 1), (8, 64, 64, 0, 5), (8, 8, 16, 0, 40), (2, 100, 16, 1, 1)):
         assert ask(*step) == "one", step
+
+
+def _random_call(rng):
+    """A call and the sizes of a smaller one with the same heads, types and blocks."""
+    H = rng.choice([1, 2, 4, 8, 8, 16, 64])
+    fixed = dict(d=rng.choice([64, 128]), g=rng.choice([1, 2, 4, 4, 7, 8, 16, 17, 40, 128]), policy=[rng.choice([0, 1, 2, 3]) for _ in range(H)],
+                 seg=rng.choice([16, 64, 512, 4096]), tail=rng.choice([0, 5, 16]), block=rng.choice([16, 48, 64, 128, 512]), e4m3=rng.random() < 0.5,
+                 out_fp32=rng.random() < 0.5)
+    log = lambda lo, hi: min(hi, max(lo, int(lo * (hi / lo) ** rng.random() + 0.5)))
+    B, longest = log(1, 300), rng.choice([1, log(1, 8), log(1, 60000)])
+    big = dict(B=B, longest=longest, total=rng.randint(longest, min(B * longest, 400000)) if B * longest > longest else longest, most=log(1, 2000000),
+               chosen=rng.choice([log(1, 64), log(1, 4096), log(1, 65536)]))
+    big["total"] = max(big["total"], longest)
+    small = dict(B=log(1, B), longest=log(1, longest), most=log(1, big["most"]), chosen=log(1, big["chosen"]))
+    small = {x: (y if rng.random() < 0.6 else big[x]) for x, y in small.items()}
+    hi = min(small["B"] * small["longest"], big["total"])
+    small["total"] = log(small["longest"], hi)
+    return fixed, big, small
+
+
+def _call_line(fixed, size):
+    new = [size["longest"]] + [0] * (size["B"] - 1)
+    return line(**fixed, new=new, total=size["total"], most=size["most"], chosen=size["chosen"])
+
+
+def test_a_workspace_covers_every_smaller_call(forms):
+    """Which forms calls take changes with their sizes; a program allocates once, for its largest.  No form lays out more than is asked for."""
+    import random
+    rng = random.Random(11)
+    calls = [_random_call(rng) for _ in range(4000)]
+    large, little = (forms([_call_line(c[0], c[i]) for c in calls]) for i in (1, 2))
+    for call, x, y in zip(calls, large, little):
+        assert x["laid_out"] <= x["asked"] and y["laid_out"] <= y["asked"] <= x["asked"] <= 2.25 * 2 ** 30, (call, x, y)
+    kinds = {(x["listed"], x["windows"]) for x in large + little}
+    assert kinds == {(x, y) for x in ("blocks", "tokens") for y in ("shares", "units", "tokens")}
+    # one batch, all of its lengths
+    for policy in ([1] * 8, [2] * 8, [3, 3, 3, 3, 1, 1, 1, 1]):
+        asked = [forms([line(d=128, g=4, policy=policy, seg=4096, tail=1024, new=[n] + [0] * (B - 1), most=131072, block=64, chosen=32)])[0]["asked"]
+                 for B, n in ((1, 1), (1, 2), (1, 64), (2, 64), (2, 512), (2, 4096), (8, 4096), (8, 8192), (8, 16384), (8, 32768))]
+        assert asked == sorted(asked), (policy, asked)
+
+
+def test_the_room_for_a_choice_covers_every_smaller_one():
+    sizes = [(n, rows, chosen) for n in (1, 17, 1000, 8192, 100000) for rows in (100, 90000, 100000, 131072, 4000000) for chosen in (4, 64)]
+    cfg = sa.make_config(batch=100000, n_q_heads=32, n_kv_heads=8, head_dim=128, seg_len=4096, tail_len=1024, kv_policy=[2] * 8)
+    pages = sa.make_pages(k=4096, v=4096, table=4096, max_pages=4000000 // 64, page_rows=64, n_pages=1)
+    blocks = sa.make_blocks(block_rows=64, bounds=4096, scale=4096)
+    need = {s: sa.seg_kv_paged_choose_workspace_bytes(cfg, pages, blocks, *s) for s in sizes}
+    for s in sizes:
+        assert need[s] > 0 and all(need[t] <= need[s] for t in sizes if all(x <= y for x, y in zip(t, s))), s
