@@ -430,8 +430,8 @@ ChosenTiles count_tiles(const PagedChosenArgs &a) {
 }
 bool many_tokens(const PagedChosenArgs &a, long long max_seqlen) { return max_seqlen > 1 && a.g <= kColumns; }
 constexpr long long kLeastPart = 2 * kChosenWaves;  // tiles
-// Windows' workgroups that are resident (D = 64: three on a compute unit).
-long long windows_resident(const PagedChosenArgs &a) { return a.D == 128 ? kResident : kResident * 3 / 2; }
+// Shares at most: as many workgroups as can be resident (D = 64: three on a compute unit, or two, by the form's registers).
+long long shares_at_most(const PagedChosenArgs &a) { return a.D == 128 ? kResident : kResident * 3 / 2; }
 // Shares that as many units can be cut into.
 long long most_shares(long long units, long long tiles, long long resident) {
   if (units >= resident) return resident;
@@ -481,7 +481,9 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
   if (a.wide_windows) {
     // Shares of equal length for as many workgroups as are resident, but where the units alone are several rounds of them, a workgroup for
     // each (8 heads with windows up to 5K, new tokens: 2048 342 us in shares and 449 by units, 8192 1041 and 1039, 16384 2105 and 2018).
-    const long long resident = windows_resident(a);
+    // The runtime is asked how many are: heads of 64, bf16 pages, fp32 outputs have two on a compute unit (2048 tokens in 768 shares 165 us, in 512
+    // 143), the other forms of 64 three.
+    const long long asked = windows_resident(a), most = shares_at_most(a), resident = asked < 8 ? kResident : asked < most ? asked / 8 * 8 : most;
     a.wide_wgs = units_other < 4 * resident ? (int)most_shares(units_other, tiles.other, resident) : 0;
     space.shares = a.wide_wgs;
   }
@@ -507,7 +509,7 @@ unsigned long long most_paged_chosen(PagedChosenArgs a, long long max_seqlen) {
   space.partials = cut < most_cut ? cut : most_cut;
   const double alone = (double)a.total * a.n_other * tiles.other;
   if (many && a.n_other > 0 && kAloneLaunches + alone * (alone_tile(a) - shared_tile(a) / a.wide_tokens) > kSharedLaunches)
-    space.shares = most_shares(a.n_other * (a.total / a.wide_tokens + a.B), tiles.other, windows_resident(a));
+    space.shares = most_shares(a.n_other * (a.total / a.wide_tokens + a.B), tiles.other, shares_at_most(a));
   const double rounds = ceil((double)a.total * a.n_past * a.passes / kResident) * ceil((double)tiles.past / kChosenWaves) * 3.2 * row_bytes(a) / 512;
   const double listed = (double)a.total * a.n_past * a.n_chosen * 16.0 * a.block_halves.d * row_bytes(a) / 8.5e6;
   if (many && a.n_past > 0 && kListedLaunches < (rounds > listed ? rounds : listed)) {

@@ -795,6 +795,18 @@ __global__ __launch_bounds__(256) void paged_listed_join_kernel(const PagedChose
 }
 
 template <int D, bool kE4m3>
+static long long resident_shares(bool fp32) {
+  static ResidentCount count[2];
+  const auto kern = fp32 ? paged_windows_kernel<D, kE4m3, true, true> : paged_windows_kernel<D, kE4m3, false, true>;
+  return count[fp32].get((const void *)kern, kWideThreads, 0);
+}
+long long windows_resident(const PagedChosenArgs &a) {
+  const bool fp32 = a.out_fp32 != 0;
+  return a.D == 128 ? (a.c.e4m3 ? resident_shares<128, true>(fp32) : resident_shares<128, false>(fp32))
+                    : (a.c.e4m3 ? resident_shares<64, true>(fp32) : resident_shares<64, false>(fp32));
+}
+
+template <int D, bool kE4m3>
 static hipError_t launch_windows(const PagedChosenArgs &a, hipStream_t st) {
   const auto kern = a.wide_wgs > 0 ? (a.out_fp32 ? paged_windows_kernel<D, kE4m3, true, true> : paged_windows_kernel<D, kE4m3, false, true>)
                                    : (a.out_fp32 ? paged_windows_kernel<D, kE4m3, true, false> : paged_windows_kernel<D, kE4m3, false, false>);

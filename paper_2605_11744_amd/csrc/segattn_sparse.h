@@ -110,6 +110,8 @@ constexpr int kListedRows = 64;
 unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, unsigned char *ws);
 // Bytes that no plan of these sizes, or of smaller ones, exceeds (of a planned call's arguments).
 unsigned long long most_paged_chosen(PagedChosenArgs a, long long max_seqlen);
+// Workgroups of the kernel for windows in shares that the device holds at once (0: could not be asked).
+long long windows_resident(const PagedChosenArgs &a);
 hipError_t launch_paged_windows(const PagedChosenArgs &a, hipStream_t st);
 hipError_t launch_paged_listed(const PagedChosenArgs &a, hipStream_t st);
 hipError_t launch_paged_chosen(const PagedChosenArgs &a, hipStream_t st);
