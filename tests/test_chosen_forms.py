@@ -101,3 +101,47 @@ def test_the_room_for_a_choice_covers_every_smaller_one():
     need = {s: sa.seg_kv_paged_choose_workspace_bytes(cfg, pages, blocks, *s) for s in sizes}
     for s in sizes:
         assert need[s] > 0 and all(need[t] <= need[s] for t in sizes if all(x <= y for x, y in zip(t, s))), s
+
+
+def test_windows_written_for_a_form_take_it(forms):
+    from test_gpu_sparse import SHARED
+    from test_gpu_sparse_forms import SHORT
+    most = lambda new, held, block: -(-max(h + n for h, n in zip(held, new)) // block) * block
+    lines, want = [], []
+    for d, g, policy, seg, tail, (new, held), kind in SHORT:
+        for e4m3 in (False, True):
+            lines.append(line(d=d, g=g, policy=policy, seg=seg, tail=tail, new=new, total=sum(new) + (len(new) > 1), most=most(new, held, 16), block=16, chosen=4, e4m3=e4m3,
+                              out_fp32=not e4m3))
+            want.append(kind)
+    for kind, d, g, out_fp32 in SHARED:
+        new, held, block = [900, 1100, 0, 1], [1990, 3500, 100, 0], kind["block"]
+        lines.append(line(d=d, g=g, policy=[1, 2, 0], seg=1000, tail=300, new=new, total=sum(new) + 2, most=most(new, [h + 1 for h in held], kind["page_rows"]), block=block,
+                          chosen=4, e4m3=kind.get("e4m3", False), out_fp32=out_fp32))
+        want.append("shares")
+    for e4m3 in (False, True):
+        lines.append(line(d=128, g=4, policy=[1, 2, 0], seg=1000, tail=300, new=[2000], most=3520, block=32, chosen=3, e4m3=e4m3))
+        lines.append(line(d=128, g=16, policy=[1, 0, 1, 1, 0, 0, 1, 1], seg=200, tail=56, new=[2044, 6], most=2240, block=64, chosen=1, e4m3=e4m3, out_fp32=not e4m3))
+        want += ["shares", "units"]
+    got = forms(lines)
+    assert [x["windows"] for x in got] == want
+
+
+def test_long_chunks_written_for_listed_blocks_take_them_once(forms):
+    from test_gpu_sparse import LONG
+    lines = []
+    for kind in LONG:
+        e4m3 = kind.get("e4m3", False)
+        new = [2600 if e4m3 else 1290, 0, 17]
+        held, page = [700, 30, 2000], kind["page_rows"]
+        lines += [line(d=128, g=2 if e4m3 else 4, policy=[2, 3], seg=64, tail=16, new=new, total=sum(new) + 3, chosen=16 if e4m3 else 8, e4m3=e4m3, out_fp32=f,
+                       most=-(-(max(h + n for h, n in zip(held, new)) + 1) // page) * page, block=kind["block"]) for f in (False, True)]
+    for d, g in ((64, 1), (64, 8), (128, 3), (128, 1)):
+        new = [2600 if g == 8 else 1290, 0, 17]
+        lines.append(line(d=d, g=g, policy=[2, 3], seg=64, tail=16, new=new, total=sum(new) + 3, chosen=16 if g == 8 else 8, most=-(-(700 + new[0] + 1) // 64) * 64, block=64))
+    assert [x["listed"] for x in forms(lines)] == ["blocks"] * len(lines)
+
+
+def test_reservations_written_for_a_form_take_it(forms):
+    from test_gpu_sparse_forms import RESERVATIONS
+    got = forms([f"reserve 3 {n} 16 9000 {per_head} {n * most // 2} {most}" for n, most in RESERVATIONS for per_head in (0, 1)])
+    assert got == ["one", "one"] + ["four"] * 6
