@@ -283,68 +283,64 @@ __global__ __launch_bounds__(64 * kChosenWaves, 2) void paged_chosen_kernel(cons
   }
 }
 
-// A wave per (token, KV head) whose window was shared out, or (each = 1) per query head of it: the parts' partials joined, `each` query heads one
-// after the other.  (One sequence's 32 heads 4.3 us with a wave each and 10.4 with four a wave, a chunk of 2.5K tokens' 63 and 26.)
+// A wave per (token, query head) whose window was shared out: the parts' partials joined.  (They are few: a window is shared out only where there
+// are fewer than kResident units.  One sequence's 32 heads 4.3 us, with four of them one after the other in a wave 10.4.)
 template <int D>
-__global__ __launch_bounds__(256) void paged_chosen_join_kernel(const PagedChosenArgs a, const int hx0, const int heads, const int each, const long long first_wg) {
+__global__ __launch_bounds__(256) void paged_chosen_join_kernel(const PagedChosenArgs a, const int hx0, const int heads, const long long first_wg) {
   constexpr int SF = D + kWsTailFloats, kLanes = D / 4, kGroups = 64 / kLanes, kBatch = 4;
   const int lane = threadIdx.x & 63;
-  const int turns = a.g / each;
-  const long long wave = (first_wg + blockIdx.x) * 4 + (threadIdx.x >> 6), u = wave / turns, token = u / heads;
+  const long long wave = (first_wg + blockIdx.x) * 4 + (threadIdx.x >> 6), u = wave / a.g, token = u / heads;
   if (token >= a.total) return;
-  const int j0 = (int)(wave - u * turns) * each;
+  const int j = (int)(wave - u * a.g);
   const int hx = hx0 + (int)(u - token * heads), h = a.head_of[hx];
   const bool past = hx < a.n_past;
   const int parts = past ? a.parts_past : a.parts_other;
   int i, n;
   if (sequence_of(a.cu, a.B, token, i, n) < 0) return;
   const int group = lane / kLanes, d = lane % kLanes * 4;
-#pragma unroll 2
-  for (int j = j0; j < j0 + each; ++j) {
-    const float *src = partial_of<D>(a, past, token, past ? hx : hx - a.n_past, 0) + j * SF;
-    float top = -INFINITY, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = group; s0 - group < parts; s0 += kGroups * kBatch) {
-      float2 ml[kBatch];
-      f32x4 y[kBatch];
+  const float *src = partial_of<D>(a, past, token, past ? hx : hx - a.n_past, 0) + j * SF;
+  float top = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = group; s0 - group < parts; s0 += kGroups * kBatch) {
+    float2 ml[kBatch];
+    f32x4 y[kBatch];
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int s = s0 + kGroups * k;
-        const float *part = src + (long long)(s < parts ? s : parts - 1) * a.g * SF;
-        ml[k] = *(const float2 *)(part + D);
-        y[k] = *(const f32x4 *)(part + d);
-      }
-      float m_new = top;
+    for (int k = 0; k < kBatch; ++k) {
+      const int s = s0 + kGroups * k;
+      const float *part = src + (long long)(s < parts ? s : parts - 1) * a.g * SF;
+      ml[k] = *(const float2 *)(part + D);
+      y[k] = *(const f32x4 *)(part + d);
+    }
+    float m_new = top;
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k)
-        if (s0 + kGroups * k < parts) m_new = fmaxf(m_new, ml[k].x);
-      const float ref = m_new == -INFINITY ? 0.f : m_new, keep = __builtin_amdgcn_exp2f(top - ref);
-      l *= keep;
-      o *= keep;
-      top = m_new;
+    for (int k = 0; k < kBatch; ++k)
+      if (s0 + kGroups * k < parts) m_new = fmaxf(m_new, ml[k].x);
+    const float ref = m_new == -INFINITY ? 0.f : m_new, keep = __builtin_amdgcn_exp2f(top - ref);
+    l *= keep;
+    o *= keep;
+    top = m_new;
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        if (s0 + kGroups * k < parts) {
-          const float wgt = __builtin_amdgcn_exp2f(ml[k].x - ref);
-          l += ml[k].y * wgt;
-          o += y[k] * wgt;
-        }
+    for (int k = 0; k < kBatch; ++k) {
+      if (s0 + kGroups * k < parts) {
+        const float wgt = __builtin_amdgcn_exp2f(ml[k].x - ref);
+        l += ml[k].y * wgt;
+        o += y[k] * wgt;
       }
     }
-    float most = top;
-#pragma unroll
-    for (int sh = kLanes; sh < 64; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
-    const float ref = most == -INFINITY ? 0.f : most, wgt = __builtin_amdgcn_exp2f(top - ref);
-    l *= wgt;
-    o *= wgt;
-#pragma unroll
-    for (int sh = kLanes; sh < 64; sh <<= 1) {
-      l += __shfl_xor(l, sh);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], sh);
-    }
-    if (lane < kLanes) store_out<D>(a, token * a.Hq + h * a.g + j, d, o, l, ref);
   }
+  float most = top;
+#pragma unroll
+  for (int sh = kLanes; sh < 64; sh <<= 1) most = fmaxf(most, __shfl_xor(most, sh));
+  const float ref = most == -INFINITY ? 0.f : most, wgt = __builtin_amdgcn_exp2f(top - ref);
+  l *= wgt;
+  o *= wgt;
+#pragma unroll
+  for (int sh = kLanes; sh < 64; sh <<= 1) {
+    l += __shfl_xor(l, sh);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], sh);
+  }
+  if (lane < kLanes) store_out<D>(a, token * a.Hq + h * a.g + j, d, o, l, ref);
 }
 
 constexpr long long kListedSpace = 1ll << 30;  // bytes of partials of listed blocks at a time
@@ -531,9 +527,8 @@ static hipError_t launch_chosen(const PagedChosenArgs &a, hipStream_t st) {
   });
   const int hx0 = a.parts_past > 1 ? 0 : a.n_past, heads = (a.parts_other > 1 ? a.Hkv : a.n_past) - hx0;
   if (e != hipSuccess || heads <= 0) return e;
-  const int each = a.total * heads < 8192 ? 1 : a.g;
-  return launch_in_parts((a.total * heads * (a.g / each) + 3) / 4, 256, [&](long long first, unsigned count) {
-    hipLaunchKernelGGL(paged_chosen_join_kernel<D>, dim3(count), dim3(256), 0, st, a, hx0, heads, each, first);
+  return launch_in_parts((a.total * heads * a.g + 3) / 4, 256, [&](long long first, unsigned count) {
+    hipLaunchKernelGGL(paged_chosen_join_kernel<D>, dim3(count), dim3(256), 0, st, a, hx0, heads, first);
   });
 }
 
