@@ -377,8 +377,8 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
   constexpr int NG = 2, kWaveColumns = 16 * NG, kWaves = kWideThreads / 64, NK = D / 32, NB = D / 16;
   constexpr int kRow = 2 * D, kTileBytes = kChosenTile * kRow;
   constexpr int kPieces = (kE4m3 ? D : 2 * D) / 16;   // 16-byte pieces of a row in memory
-  // of a tile's keys and values, per thread (fewer pieces than threads: the others have none)
-  constexpr int NP = (2 * kChosenTile * kPieces + kWideThreads - 1) / kWideThreads;
+  constexpr int kHalf = 16 * kPieces;                           // of 16 rows: one, two or four waves' or all threads'
+  constexpr int NP = 2 * kChosenTile * kPieces / kWideThreads;  // of a tile's keys and values, per thread
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int quad = lane >> 4, col = lane & 15;
   __shared__ __attribute__((aligned(1024))) unsigned char tiles[2][2 * kTileBytes];
@@ -458,34 +458,29 @@ __global__ __launch_bounds__(kWideThreads, 2) void paged_windows_kernel(const Pa
       u32x4 x[NP];
       int scale[NP];
     } flight0, flight1;
-    auto piece_of = [&](int p, int &row, int &half) __attribute__((always_inline)) {
-      const int first = p * kWideThreads + 64 * wave;
-      row = (first + lane) / kPieces % kChosenTile;
-      half = first / (16 * kPieces) % 2;
-      return first >= kChosenTile * kPieces;
-    };
-    const bool loads = 64 * wave < 2 * kChosenTile * kPieces;
+    // (of the four halves of keys and values; all pieces of a thread lie in one row of them)
+    auto half_of = [&](int p) __attribute__((always_inline)) { return p * (kWideThreads / kHalf) + (kHalf < kWideThreads ? wave / (kHalf / 64) : 0); };
+    const int in_half = tid / kPieces % 16, piece = tid % kPieces;
+    const unsigned in_memory = (unsigned)in_half * (unsigned)a.c.row_bytes + piece * 16;
     auto fetch = [&](Flight &f, int j) __attribute__((always_inline)) {
-      if (!loads) return;
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        int row, half;
-        const bool is_v = piece_of(p, row, half);
+        const int half = half_of(p) % 2;
+        const bool is_v = half_of(p) >= 2;
         const unsigned char *src = (is_v ? pool_v : pool_k) + of_lane(half_at, 2 * j + half);
-        f.x[p] = *(const u32x4 *)(src + (unsigned)(row & 15) * (unsigned)a.c.row_bytes + lane % kPieces * 16);
-        if constexpr (kE4m3) f.scale[p] = (is_v ? scale_v : scale_k)[of_lane(half_place, 2 * j + half) + (row & 15)];
+        f.x[p] = *(const u32x4 *)(src + in_memory);
+        if constexpr (kE4m3) f.scale[p] = (is_v ? scale_v : scale_k)[of_lane(half_place, 2 * j + half) + in_half];
       }
     };
     auto stage = [&](const Flight &f, int buf, unsigned valid, bool mixed) __attribute__((always_inline)) {
       bool bad = false;
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        if (!loads) break;
-        int row, half;
-        const bool is_v = piece_of(p, row, half);
+        const int row = half_of(p) % 2 * 16 + in_half;
+        const bool is_v = half_of(p) >= 2;
         unsigned char *dst = tiles[buf] + (is_v ? kTileBytes : 0);
-        if (is_v && (mixed || valid != ~0u)) bad |= stage_piece<D, kE4m3>(dst, row, lane % kPieces, f.x[p], f.scale[p], true, !((valid >> row) & 1), mixed);
-        else stage_piece<D, kE4m3>(dst, row, lane % kPieces, f.x[p], f.scale[p], is_v, false, false);
+        if (is_v && (mixed || valid != ~0u)) bad |= stage_piece<D, kE4m3>(dst, row, piece, f.x[p], f.scale[p], true, !((valid >> row) & 1), mixed);
+        else stage_piece<D, kE4m3>(dst, row, piece, f.x[p], f.scale[p], is_v, false, false);
       }
       if (mixed) {
         const bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
