@@ -440,9 +440,15 @@ struct Team {
 template <int kWaves, int kHeld = 8, typename Keys>
 __device__ __attribute__((always_inline)) void pick_blocks(const Keys keys, int first, int hi, int picks, int *out, Team<kWaves> &sm, int wave) {
   const int lane = threadIdx.x & 63, me = wave * 64 + lane;
+  // (one wave: its LDS accesses are done in order, but the compiler has to leave them so -- what another lane writes, it sees no reason for)
   const auto meet = [] {
-    if constexpr (kWaves > 1) __syncthreads();
-    else __builtin_amdgcn_wave_barrier();
+    if constexpr (kWaves > 1) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
   };
   // this wave's run, in whole rounds of 64 blocks
   const int rounds = (hi - first + 64 * kWaves - 1) / (64 * kWaves);
