@@ -551,8 +551,10 @@ segattn_status seg_kv_paged_release(const segattn_config *cfg, const segattn_pag
  * is at most B * max_seqlen), and the tokens' rows have been appended: token i of
  * the m of sequence b is row r = rows[b,h] - m + i of head h, and sees no row behind its own.  max_rows (host, <= max_pages *
  * page_rows): the most rows of a head; it sizes launches and workspaces, and of a head that holds more only the first
- * max_rows are seen.  At most 128 query heads per KV head.  What a call writes, its workspace among it, shares no byte with its other
- * arrays (SEGATTN_EINVAL; of the pool's K and V the caller sees to that). */
+ * max_rows are seen (a token whose row lies behind them is taken for the last of them, its window with it).  At most 128 query heads per
+ * KV head; chunks with more than 16 are taken token by token.  A workspace whose size was asked for the largest total, max_seqlen,
+ * max_rows, n_chosen and batch that a program uses serves its smaller calls too (with the same heads, types and blocks).  What a call
+ * writes, its workspace among it, shares no byte with its other arrays (SEGATTN_EINVAL; of the pool's K and V the caller sees to that). */
 typedef struct {
   int32_t block_rows;     /* a multiple of 16 that divides page_rows; 64 is a good size           */
   int8_t *bounds;         /* device, 16-byte aligned, [n_pages][heads][page_rows / block_rows][2][D]: upper, then lower

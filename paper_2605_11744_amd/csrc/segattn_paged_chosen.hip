@@ -8,8 +8,8 @@
 // P enters as two bf16 (what that leaves is below 2^-16 of a weight), for fp32 outputs as three: the matrix pipes idle beside the memory.
 // K and V go from memory to LDS through registers, a tile ahead, because the halves lie anywhere and 8-bit rows become bf16 on the way.  Bound by
 // memory where the workgroups fill the card (48 sequences of 8-bit rows, two heads with 32 blocks of 64 and six with windows up to 5K rows:
-// 58 us, 4.7 TB/s; without the windows' unequal lengths 6.3 to 6.7), else by the latency of a round of tiles, 1.2 us, and 9 us
-// around them (one sequence's 64 blocks: 9 us and 4 to join).
+// 58 us, 4.7 TB/s, of bf16 rows 98 us, 5.5 TB/s; without the windows' unequal lengths 6.3 to 6.7), else by latencies: row count -> list -> page ->
+// tile, a second round of tiles, the waves' merge (one sequence's 64 blocks: 9 us and 4 to join).
 #include <math.h>
 
 #include <type_traits>
@@ -377,9 +377,9 @@ double shared_tile(const PagedChosenArgs &a) { return (1.8 + row_bytes(a) / 512)
 
 // Whether the windows of several tokens a sequence share their tiles, by how long both ways take (us, with the longest window's tiles): 128 columns
 // cost what they cost however few of them are tokens', but single tokens read the rows anew, from the caches if that.  Measured, alone and
-// shared, in us, windows up to 5K rows: a 130K history, eight heads, 4 tokens 16 and 31, 16 tokens 27 and 37, 32 tokens 40 and 40, 64 tokens 60 and
-// 43; 48 sequences of 8-bit rows, six heads of eight, 2 tokens 113 and 164, 3 tokens 157 and 172, 4 tokens 200 and 175 (bf16 rows: 186
-// and 184, 270 and 206 for three); eight of them, 4 tokens 45 and 57, 8 tokens 68 and 62.
+// shared, in us, windows up to 5K rows: a 130K history, eight heads, 4 tokens 16 and 31, 16 tokens 27 and 36, 32 tokens 40 and 39, 64 tokens 60 and
+// 42; 48 sequences of 8-bit rows, six heads of eight, 2 tokens 114 and 158, 3 tokens 158 and 167, 4 tokens 201 and 172 (bf16 rows: 186
+// and 174, 272 and 197 for three); eight of them, 4 tokens 45 and 55, 8 tokens 68 and 61.
 bool windows_share_tiles(const PagedChosenArgs &a, double tiles) {
   const double bytes = row_bytes(a), alone = (double)a.total * a.n_other * tiles;
   const double shared = (double)a.n_other * (a.cu ? (double)a.total / a.wide_tokens + a.B : (double)a.total) * tiles;
@@ -476,7 +476,7 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
   if (a.parts_other > 1) space.partials += (unsigned long long)a.total * a.n_other * a.parts_other;
   if (a.wide_windows) {
     // Shares of equal length for as many workgroups as are resident, but where the units alone are several rounds of them, a workgroup for
-    // each (8 heads with windows up to 5K, new tokens: 2048 342 us in shares and 449 by units, 8192 1041 and 1039, 16384 2105 and 2018).
+    // each (8 heads with windows up to 5K, up to as many new tokens: 2048 326 us in shares and 454 by units, 8192 991 and 975, 16384 1998 and 1901).
     // The runtime is asked how many are: heads of 64, bf16 pages, fp32 outputs have two on a compute unit (2048 tokens in 768 shares 165 us, in 512
     // 143), the other forms of 64 three.
     const long long asked = windows_resident(a), most = shares_at_most(a), resident = asked < 8 ? kResident : asked < most ? asked / 8 * 8 : most;

@@ -1,5 +1,5 @@
 // seg_attn_paged_chosen, many tokens at a time: the waves of a workgroup share keys and values in LDS, and each has query columns of
-// its own, 32 of them, in the arithmetic of the kernel for single tokens.
+// its own, 32 of them (16 for listed blocks), in the arithmetic of the kernel for single tokens.
 //
 // Windows: the columns are the query heads of neighbouring tokens, the rows all that one of them sees.  Listed blocks, where
 // the tokens of a sequence are so many that a block is listed by several of them: the columns are the heads of tokens that
@@ -7,9 +7,9 @@
 // (token, entry) leaves a partial (acc[D], m, l) per query head, and a last launch joins a token's partials.  Which
 // token lands in which column depends on the order of atomics, but no column's numbers depend on its neighbours.
 //
-// A chunk of 2533 tokens behind up to 60K rows, eight KV heads of four query heads, half of them long-range with 32 blocks of 64 rows: windows 194 us
-// and 16 to join (73 GFLOP, 375 TFLOP/s: eight waves a compute unit do not hide a tile's chain of scores, maximum, exponentials and products),
-// listed blocks 221 (0.68 GB of partials written, 3.1 TB/s), their join 118 (read, 5.7 TB/s), turning the lists round 41.
+// A chunk of 2533 tokens behind up to 60K rows, eight KV heads of four query heads, half of them long-range with 32 blocks of 64 rows: windows 185 us
+// and 16 to join (73 GFLOP, 395 TFLOP/s: eight waves a compute unit do not hide a tile's chain of scores, maximum, exponentials and products),
+// listed blocks 221 (0.68 GB of partials written, 3.1 TB/s), their join 119 (read, 5.7 TB/s), turning the lists round 40.
 #include "segattn_paged_chosen.h"
 
 namespace segattn {
@@ -303,7 +303,7 @@ __device__ inline WindowUnit window_unit(const PagedChosenArgs &a, long long u) 
 }
 // The units' tiles, one unit after the other, are cut into shares of one length, a workgroup each: windows are of all lengths, and with a
 // workgroup for each of them, or for halves, the part waits for the longest (2500 tokens, four heads with windows up to 5K: 281 us and 26 to
-// join in halves, 200 and 17 in shares).  Each workgroup finds its own: the threads sum up the units' costs, then lanes search the units
+// join in halves, 185 and 16 in shares).  Each workgroup finds its own: the threads sum up the units' costs, then lanes search the units
 // of the thread in whose sum the share begins.
 struct WindowShare {
   long long unit, at;     // the first unit, and where it begins in the order of all tiles
@@ -629,7 +629,7 @@ __global__ __launch_bounds__(256) void paged_windows_join_kernel(const PagedChos
 
 // ---- listed blocks ------------------------------------------------------------------------------
 // A task: some of the entries that name one block.  Its rows go to LDS kListedRows at a time (a partial for each such piece of a
-// block), and the waves take the columns 32 at a time.
+// block), and the waves take the columns 16 at a time.
 template <int D, bool kE4m3, bool kFp32>
 __global__ __launch_bounds__(kListedThreads, 4) void paged_listed_kernel(const PagedChosenArgs a, const long long first_wg) {
   constexpr int NG = 1, kWaveColumns = 16 * NG, NK = D / 32, NB = D / 16;
