@@ -479,7 +479,8 @@ unsigned long long plan_paged_chosen(PagedChosenArgs &a, long long max_seqlen, u
     // each (8 heads with windows up to 5K, up to as many new tokens: 2048 326 us in shares and 454 by units, 8192 991 and 975, 16384 1998 and 1901).
     // The runtime is asked how many are: heads of 64, bf16 pages, fp32 outputs have two on a compute unit (2048 tokens in 768 shares 165 us, in 512
     // 143), the other forms of 64 three.
-    const long long asked = windows_resident(a), most = shares_at_most(a), resident = asked < 8 ? kResident : asked < most ? asked / 8 * 8 : most;
+    // (Without a workspace the question is only how large one may be: nothing is asked.)
+    const long long most = shares_at_most(a), asked = ws ? windows_resident(a) : most, resident = asked < 8 ? kResident : asked < most ? asked / 8 * 8 : most;
     a.wide_wgs = units_other < 4 * resident ? (int)most_shares(units_other, tiles.other, resident) : 0;
     space.shares = a.wide_wgs;
   }
